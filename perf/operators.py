@@ -7,8 +7,9 @@ computes the plain form in 32 bits, or, with `own`, makes the library's calls; `
 
 Definitions.
   4-bit rows: every 32 dimensions of a head have a scale s = bf16((max - min) / 15) and a base b = bf16(min - 16 s); an element x is
-  held as c = min(max(rint((x - b) / s) - 16, 0), 15) (0 where s is 0) and stands for bf16(b + (16 + c) s).  A page of a head is
-  64 rows of codes, then 64 rows of (s, b) pairs; dimension d of a row is bits 4 (d % 8 / 2) + 16 (d % 2) of its 32-bit word d / 8.
+  held as c = min(max(rint((x - b) / s) - 16, 0), 15) (0 where s is 0) and stands for bf16(b + (16 + c) s).  A page of a head is, for
+  every group of 32 dimensions, 64 rows of 16 bytes of codes, and then 64 rows of (s, b) pairs, one for each group; element e of a row
+  of codes is bits 4 (e % 8 / 2) + 16 (e % 2) of its 32-bit word e / 8.
   Attention: a sequence with n cached positions has k causal slots at n .. n + k - 1 (their K and V are in its pages) and, unless
   the call is causal, k blocks of k mask slots.  Causal slot j is at position n + j and sees positions <= n + j; slot i of block b is
   at position n + b + 1 + i and sees positions <= n + b and its own block's k local rows.  With a window w > 0 a slot at position p
@@ -128,10 +129,10 @@ def _values(c, s, b):
 
 def _pack(c, s, b):
     """Codes and (scale, base) of a page [..., 64, groups, 32] as the bytes of its record."""
-    w = c.flatten(-2).to(torch.int64).unflatten(-1, (-1, 4, 2))           # [..., words, pair, which of it]
+    w = c.transpose(-2, -3).to(torch.int64).unflatten(-1, (-1, 4, 2))     # [..., group, row, word, pair, which of it]
     at = torch.tensor([[4 * i + 16 * j for j in range(2)] for i in range(4)], device=c.device)
     w = (w << at).sum((-1, -2))
-    codes = torch.where(w >= 1 << 31, w - (1 << 32), w).to(torch.int32).contiguous().view(torch.uint8).flatten(-2)
+    codes = torch.where(w >= 1 << 31, w - (1 << 32), w).to(torch.int32).contiguous().view(torch.uint8).flatten(-3)
     pairs = torch.stack([s, b], -1).bfloat16().contiguous().view(torch.uint8).flatten(-3)
     return torch.cat([codes, pairs], -1)
 
@@ -139,9 +140,9 @@ def _pack(c, s, b):
 def _unpack(pool, hd):
     """The values that the records [..., bytes] of a pool stand for, [..., 64, hd] in bf16."""
     n = PAGE * hd // 2
-    w = pool[..., :n].contiguous().view(torch.int32).unflatten(-1, (PAGE, hd // 8))
+    w = pool[..., :n].contiguous().view(torch.int32).unflatten(-1, (hd // GROUP, PAGE, GROUP // 8)).transpose(-2, -3)
     at = torch.tensor([4 * i + 16 * j for i in range(4) for j in range(2)], device=pool.device, dtype=torch.int32)
-    c = ((w[..., None] >> at) & 15).flatten(-2).unflatten(-1, (-1, GROUP)).float()
+    c = ((w[..., None] >> at) & 15).flatten(-2).float()
     sb = pool[..., n:].contiguous().view(torch.bfloat16).unflatten(-1, (PAGE, hd // GROUP, 2)).float()
     return _values(c, sb[..., 0], sb[..., 1])
 
@@ -338,7 +339,7 @@ def _stored(x):
 def _read(pool, page, hd):
     """The rows [head, 64, hd] of one page of 4-bit records."""
     rec = pool[page]
-    raw = rec[:, :PAGE * hd // 2].reshape(-1, PAGE, hd // 8, 4).long()
+    raw = rec[:, :PAGE * hd // 2].reshape(-1, hd // GROUP, PAGE, GROUP // 8, 4).permute(0, 2, 1, 3, 4).reshape(-1, PAGE, hd // 8, 4).long()
     word = raw[..., 0] + (raw[..., 1] << 8) + (raw[..., 2] << 16) + (raw[..., 3] << 24)
     code = torch.stack([(word >> (4 * (d // 2) + 16 * (d % 2))) & 15 for d in range(8)], -1).flatten(-2).double()
     sb = rec[:, PAGE * hd // 2:].contiguous().view(torch.bfloat16).reshape(-1, PAGE, hd // GROUP, 2).double().repeat_interleave(GROUP, 2)
