@@ -368,6 +368,78 @@ int tidar_gemm(tidar_ctx *ctx, const void *A, const void *W, int32_t R, int32_t 
  * calls since the last check are then invalid).                                        */
 int tidar_sync(tidar_ctx *ctx);
 
+/* ---- a paged cache that the caller keeps ----------------------------------------------
+ * For programs that hold their own K/V pages next to the library, as tidar_attention's callers do: the page map of a
+ * batch made on the device, pages in 4 bits, and attention over 4-bit or bf16 pages with a sliding window.  All pointers
+ * are DEVICE pointers; everything is enqueued on the context's stream and can be captured into a graph there.  The calls of
+ * one context use its scratch: graphs captured from it, and calls of it, must not overlap on the GPU.
+ * Nothing is synchronised (see tidar_sync).  Errors: EINVAL (nothing is launched), ECUDA.       */
+
+/* Bytes of one page of one KV head in 4 bits: 64 * (head_dim/2 + head_dim/32*4).  A pool is [n_pages][n_kv_heads][bytes].
+ * Every 32 dimensions of a row of a head have a scale s = bf16((max - min) / 15) and a base b = bf16(min - 16 s), both
+ * rounded to nearest; an element x is held as the code c = min(max(rint((x - b) / s) - 16, 0), 15) (0 where s is 0) and
+ * stands for bf16(b + (16 + c) s).  What is held is finite: NaN counts as 0, and magnitudes above 2^126 as 2^126.
+ * A record: for each group of 32 dimensions 64 rows of 16 bytes of codes (element e of the group: bits 4 (e % 8 / 2) + 16 (e % 2)
+ * of the row's little-endian 32-bit word e / 8), then 64 rows of head_dim/32 pairs (s, b) of bf16.                                             */
+int tidar_kv4_page_bytes(int32_t head_dim, size_t *out_bytes);
+
+/* Page tables and slots for the rows that sequences are about to get, from lengths on the device (no host round trip
+ * between a step that settles tokens and the next).
+ *   seq_len [n_seqs]  positions cached; negative: no such sequence (a padded batch), nothing is done for it
+ *   n_new [n_seqs]    rows to come, at positions seq_len .. seq_len + n_new - 1 (negative counts as 0)
+ *   held [n_seqs]     entries of the sequence's row of the table that are backed by pages already (may be more than the
+ *                     length needs: a step that drafted further than it accepted)
+ *   free_pages [n_free], free_begin [1] (or NULL: 0)  pages nobody holds, and how many of them are used up
+ *   page_table [n_seqs][pages_per_seq]  entries [held, ceil((seq_len + n_new) / 64)) are written: free pages in order,
+ *                     sequence after sequence, and -1 once the list has run out; all others are left as they are
+ *   held_out [n_seqs] max(held, entries that are needed)
+ *   row_start [n_seqs + 1]  first row of every sequence, and the number of rows
+ *   slots [max_rows]  64 * page + place of every row, sequence after sequence; -1 for a row without a page (list or
+ *                     table exhausted) and behind the last row
+ *   counts [3]        free_begin for the next call (beyond n_free: that many pages are missing), rows without a slot, rows
+ * held_out may be held, and counts may be free_begin; no other arrays may overlap.  Sums saturate at 2^31 - 1.
+ * Needs 1 <= n_seqs <= 4096.                                                                     */
+int tidar_page_map(tidar_ctx *ctx, const int32_t *seq_len, const int32_t *n_new, const int32_t *held, int32_t n_seqs, const int32_t *free_pages, int32_t n_free,
+                   const int32_t *free_begin, int32_t *page_table, int32_t pages_per_seq, int32_t *held_out, int32_t *row_start, int32_t *slots,
+                   int32_t max_rows, int32_t *counts);
+
+/* Rows of K and V ([n_rows][n_kv_heads][head_dim] bf16, row strides in elements, multiples of 8) into 4-bit pages at
+ * `slots` (tidar_page_map's); a slot outside [0, 64 n_pages) skips its row.  A slot may be named once: what it holds
+ * after two rows were sent there is not defined.                                                */
+int tidar_kv4_store(tidar_ctx *ctx, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *slots, int32_t n_rows,
+                    void *k_pages, void *v_pages, int32_t n_pages);
+/* The values that the listed slots stand for, as rows; a row whose slot is outside the pool is left as it is.  */
+int tidar_kv4_load(tidar_ctx *ctx, const void *k_pages, const void *v_pages, int32_t n_pages, const int32_t *slots, int32_t n_rows,
+                   void *k, int64_t k_stride, void *v, int64_t v_stride);
+
+/* Attention of a step, or of causal rows alone, over pages that the caller keeps, with a sliding window.
+ *   q        [n_seqs*T][n_q_heads][head_dim] bf16; q_stride: elements from row to row (0 = contiguous; a multiple of 8), so that
+ *            q can be a part of the QKV projection's output
+ *   k_pages, v_pages [n_pages][n_kv_heads][...]: 4-bit records (tidar_attention_kv4) or bf16 [64][head_dim] (tidar_attention_window)
+ *   page_table [n_seqs][pages_per_seq], seq_len [n_seqs] = n: the positions n .. n+k-1 of the k causal slots are in the pages too
+ *   k_local, v_local [n_seqs*k*k][n_kv_heads][head_dim] bf16, local_stride as q_stride: K/V of the mask slots.  With them a
+ *            sequence has T = k*(k+1) rows in the slot order of a decode step; both NULL: T = k causal rows and nothing else
+ *            (k = 1: one token per sequence; larger: a chunk of a prompt, as many rows as the context has room for)
+ *   out      [n_seqs*T][n_q_heads*head_dim] bf16
+ *   window, sinks: causal slot j is at position p = n + j and sees positions t <= n + j; mask slot i of block b is at position
+ *            p = n + b + 1 + i and sees positions t <= n + b and its block's k local rows.  With window > 0, of the positions t only
+ *            those with t < sinks or t > p - window (local rows are always seen).  window = 0: all of them
+ * A sequence of negative length is absent: its rows of out stay as they are.  Lengths are clamped to pages_per_seq*64 - k.  A
+ * page entry outside [0, n_pages) is seen by no row; a row that sees nothing is 0.  Positions that no row of the call
+ * sees may hold anything, NaN included; V of positions that some row sees must be finite (K too with bf16 pages).
+ * Uses the context's head layout, stream, implementation choice and scratch.                    */
+typedef struct {
+  const void *q; int64_t q_stride;
+  const void *k_pages, *v_pages; int32_t n_pages;
+  const int32_t *page_table; int32_t pages_per_seq;
+  const int32_t *seq_len;
+  const void *k_local, *v_local; int64_t local_stride;
+  void *out;
+  int32_t n_seqs, k, window, sinks;
+} tidar_attention_args;
+int tidar_attention_kv4(tidar_ctx *ctx, const tidar_attention_args *args);
+int tidar_attention_window(tidar_ctx *ctx, const tidar_attention_args *args);
+
 /* ---- structured-mask attention for callers that cannot allocate ---------------------
  * (The paper has no counterpart: this is a packaging variant of tidar_attention.)
  * Same mask, same tensor layouts and the same result (within rounding) as

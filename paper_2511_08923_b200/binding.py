@@ -44,6 +44,12 @@ class tidar_weights(C.Structure):
                                                      "bqkv", "q_norm", "k_norm")]
 
 
+class tidar_attention_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("n_pages", C.c_int32),
+                ("page_table", C.c_void_p), ("pages_per_seq", C.c_int32), ("seq_len", C.c_void_p), ("k_local", C.c_void_p), ("v_local", C.c_void_p),
+                ("local_stride", C.c_int64), ("out", C.c_void_p)] + [(n, C.c_int32) for n in ("n_seqs", "k", "window", "sinks")]
+
+
 _lib = None
 
 
@@ -86,6 +92,12 @@ def load(rebuild: bool = False) -> C.CDLL:
         "tidar_debug_set_timing": (C.c_int, [ctxp, I32]),
         "tidar_debug_get_timing": (C.c_int, [ctxp, P(C.c_float)]),
         "tidar_attention": (C.c_int, [ctxp, VP, VP, VP, I32, VP, I32, VP, VP, VP, VP, I32, I32]),
+        "tidar_kv4_page_bytes": (C.c_int, [I32, P(C.c_size_t)]),
+        "tidar_page_map": (C.c_int, [ctxp, VP, VP, VP, I32, VP, I32, VP, VP, I32, VP, VP, VP, I32, VP]),
+        "tidar_kv4_store": (C.c_int, [ctxp, VP, C.c_int64, VP, C.c_int64, VP, I32, VP, VP, I32]),
+        "tidar_kv4_load": (C.c_int, [ctxp, VP, VP, I32, VP, I32, VP, C.c_int64, VP, C.c_int64]),
+        "tidar_attention_kv4": (C.c_int, [ctxp, P(tidar_attention_args)]),
+        "tidar_attention_window": (C.c_int, [ctxp, P(tidar_attention_args)]),
         "tidar_gemm": (C.c_int, [ctxp, VP, VP, I32, I32, I32, I32, VP]),
         "tidar_sync": (C.c_int, [ctxp]),
         "tidar_attention_static": (C.c_int, [VP, VP, VP, I32, VP, I32, VP, VP, VP, VP, I32, I32, I32, I32, I32, VP]),
@@ -395,6 +407,107 @@ class Tidar:
         self._check(self.lib.tidar_attention(
             self.ctx, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0], page_table.data_ptr(), page_table.shape[1],
             seq_len.data_ptr(), k_local.data_ptr(), v_local.data_ptr(), out.data_ptr(), n_seqs, k))
+
+    # -- a paged cache that the caller keeps -----------------------------------
+    def _tensor(self, name, x, dtype, shape, row_strided=False):
+        """Checks a caller's tensor (its device, type, shape, layout) and returns its address; a None in `shape` stands for any size."""
+        if not isinstance(x, torch.Tensor):
+            raise ValueError(f"{name} must be a tensor")
+        if x.device.type != "cuda" or (self.device.index is not None and x.device.index != self.device.index):
+            raise ValueError(f"{name} is on {x.device}, the context on {self.device}")
+        if x.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}, not {x.dtype}")
+        if x.dim() != len(shape) or any(b is not None and a != b for a, b in zip(x.shape, shape)):
+            raise ValueError(f"{name} must have shape {tuple('any' if b is None else b for b in shape)}, not {tuple(x.shape)}")
+        inner = x[0] if row_strided and x.shape[0] else x
+        if not inner.is_contiguous() or (row_strided and x.shape[0] > 1 and x.stride(0) < inner.numel()):
+            raise ValueError(f"{name} must be contiguous" + (" within a row, its rows apart" if row_strided else ""))
+        return x.data_ptr()
+
+    @staticmethod
+    def _row_stride(x):
+        return x.stride(0) if x.shape[0] > 1 else x[0].numel() if x.shape[0] else x.shape[1] * x.shape[2]
+
+    def page_map(self, seq_len, n_new, held, free_pages, page_table, held_out, row_start, slots, counts, free_begin=None):
+        """Page table entries and slots for the rows that sequences are about to get (see tidar_page_map).
+
+        int32 device tensors: ``seq_len``, ``n_new``, ``held``, ``held_out`` [n_seqs], ``free_pages`` [n_free], ``page_table``
+        [n_seqs, pages_per_seq], ``row_start`` [n_seqs + 1], ``slots`` [max_rows], ``counts`` [3], ``free_begin`` [1] or None
+        (``counts[:1]`` of the call before)."""
+        i32, B = torch.int32, seq_len.shape[0]
+        p = {n: self._tensor(n, x, i32, sh) for n, x, sh in (
+            ("seq_len", seq_len, (B,)), ("n_new", n_new, (B,)), ("held", held, (B,)), ("free_pages", free_pages, (None,)), ("page_table", page_table, (B, None)),
+            ("held_out", held_out, (B,)), ("row_start", row_start, (B + 1,)), ("slots", slots, (None,)), ("counts", counts, (3,)))}
+        begin = None if free_begin is None else self._tensor("free_begin", free_begin, i32, (1,))
+        with torch.cuda.device(self.device):
+            self._check(self.lib.tidar_page_map(self.ctx, p["seq_len"], p["n_new"], p["held"], B, p["free_pages"], free_pages.shape[0], begin, p["page_table"],
+                                                page_table.shape[1], p["held_out"], p["row_start"], p["slots"], slots.shape[0], p["counts"]))
+
+    def _kv4_rows(self, k, v, slots, k_pages, v_pages):
+        hkv, hd, rows = self.shape.n_kv_heads, self.shape.head_dim, slots.shape[0]
+        pool = (k_pages.shape[0], hkv, kv4_page_bytes(hd))
+        return (self._tensor("k", k, torch.bfloat16, (rows, hkv, hd), True), self._row_stride(k), self._tensor("v", v, torch.bfloat16, (rows, hkv, hd), True), self._row_stride(v),
+                self._tensor("slots", slots, torch.int32, (rows,)), rows, self._tensor("k_pages", k_pages, torch.uint8, pool), self._tensor("v_pages", v_pages, torch.uint8, pool), pool[0])
+
+    def kv4_store(self, k, v, slots, k_pages, v_pages):
+        """Rows of K and V [rows, n_kv_heads, head_dim] (rows may be strided) into 4-bit pages (see tidar_kv4_store)."""
+        pk, sk, pv, sv, ps, rows, kp, vp, n = self._kv4_rows(k, v, slots, k_pages, v_pages)
+        if rows == 0:
+            return
+        with torch.cuda.device(self.device):
+            self._check(self.lib.tidar_kv4_store(self.ctx, pk, sk, pv, sv, ps, rows, kp, vp, n))
+
+    def kv4_load(self, k_pages, v_pages, slots, k, v):
+        """The values that slots of 4-bit pages stand for, into rows of K and V (see tidar_kv4_load)."""
+        pk, sk, pv, sv, ps, rows, kp, vp, n = self._kv4_rows(k, v, slots, k_pages, v_pages)
+        if rows == 0:
+            return
+        with torch.cuda.device(self.device):
+            self._check(self.lib.tidar_kv4_load(self.ctx, kp, vp, n, ps, rows, pk, sk, pv, sv))
+
+    def _attention_cache(self, entry, record, dtype, q, k_pages, v_pages, page_table, seq_len, k_local, v_local, out, n_seqs, k, window, sinks):
+        hq, hkv, hd = self.shape.n_q_heads, self.shape.n_kv_heads, self.shape.head_dim
+        blocks = k_local is not None or v_local is not None
+        rows, n_pages = n_seqs * k * (k + 1 if blocks else 1), k_pages.shape[0]
+        a = tidar_attention_args(
+            q=self._tensor("q", q, torch.bfloat16, (rows, hq, hd), True), q_stride=self._row_stride(q),
+            k_pages=self._tensor("k_pages", k_pages, dtype, (n_pages, hkv) + record), v_pages=self._tensor("v_pages", v_pages, dtype, (n_pages, hkv) + record), n_pages=n_pages,
+            page_table=self._tensor("page_table", page_table, torch.int32, (n_seqs, None)), pages_per_seq=page_table.shape[1],
+            seq_len=self._tensor("seq_len", seq_len, torch.int32, (n_seqs,)), out=self._tensor("out", out, torch.bfloat16, (rows, hq * hd)),
+            n_seqs=n_seqs, k=k, window=window, sinks=sinks)
+        if blocks:
+            a.k_local, a.v_local = (self._tensor(n, x, torch.bfloat16, (n_seqs * k * k, hkv, hd), True) for n, x in (("k_local", k_local), ("v_local", v_local)))
+            a.local_stride = self._row_stride(k_local)
+            if self._row_stride(v_local) != a.local_stride:
+                raise ValueError("k_local and v_local must have the same row stride")
+        with torch.cuda.device(self.device):
+            self._check(entry(self.ctx, C.byref(a)))
+
+    def attention_kv4(self, q, k_pages, v_pages, page_table, seq_len, k_local, v_local, out, n_seqs: int, k: int, window: int = 0, sinks: int = 0):
+        """Attention over 4-bit pages, of a step (with local rows) or of causal rows alone (k_local = v_local = None; k = 1: one token
+        per sequence), within a window if window > 0 (see tidar_attention_kv4).  Rows of q and of the local tensors may be strided."""
+        self._attention_cache(self.lib.tidar_attention_kv4, (kv4_page_bytes(self.shape.head_dim),), torch.uint8, q, k_pages, v_pages, page_table, seq_len,
+                              k_local, v_local, out, n_seqs, k, window, sinks)
+
+    def attention_window(self, q, k_pages, v_pages, page_table, seq_len, k_local, v_local, out, n_seqs: int, k: int, window: int, sinks: int = 0):
+        """The same over bf16 pages [n_pages, n_kv_heads, 64, head_dim] (see tidar_attention_window)."""
+        self._attention_cache(self.lib.tidar_attention_window, (64, self.shape.head_dim), torch.bfloat16, q, k_pages, v_pages, page_table, seq_len,
+                              k_local, v_local, out, n_seqs, k, window, sinks)
+
+
+def kv4_page_bytes(head_dim: int) -> int:
+    """Bytes of one page of one KV head in 4 bits (see tidar_kv4_page_bytes)."""
+    n = C.c_size_t(0)
+    lib = load()
+    rc = lib.tidar_kv4_page_bytes(head_dim, C.byref(n))
+    if rc:
+        raise TidarError(rc, (lib.tidar_last_error(None) or b"").decode())
+    return n.value
+
+
+def kv4_pages(n_pages: int, n_kv_heads: int, head_dim: int, device="cuda:0") -> torch.Tensor:
+    """An empty pool of 4-bit pages for K or V."""
+    return torch.zeros(n_pages, n_kv_heads, kv4_page_bytes(head_dim), dtype=torch.uint8, device=device)
 
 
 def plan_ks(n_seqs: int, k_max: int, row_budget: int = 0, want: Optional[Sequence[int]] = None) -> List[int]:

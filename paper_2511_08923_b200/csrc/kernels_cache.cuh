@@ -1,0 +1,319 @@
+// A paged cache that the caller keeps: page map of a batch, K and V rows held in 4 bits, and the plain attention over such pages or bf16
+// pages with a sliding window.
+#pragma once
+#include "common.cuh"
+
+// ---- rows in 4 bits --------------------------------------------------------------------
+// Every 32 dimensions of a head (a group) have a scale s = bf16((max - min) / 15) and a base b = bf16(min - 16 s).  An element is held as
+// a code c in 0 .. 15 and stands for bf16(b + (16 + c) s).  The base lies 16 scales below the minimum because 16 + c is a bf16 number whose
+// mantissa holds c: (code << 3) | 0x4180 is that number, so a reader gets from codes to values with one shift, one logical operation and one
+// packed FMA for two of them, and no subtraction.  (Rounding such a base costs at most 2^-9 of about 24 s for centred groups: 0.05 s.)
+// A page of a head is one record: for each group 64 rows of 16 bytes of codes, then 64 rows of (s, b) pairs.  Element e of a group is bits
+// 4 (e % 8 / 2) + 16 (e % 2) of the row's 32-bit word e / 8, so that a shift brings two neighbours to the places of a pair of bf16 numbers; and
+// lanes that take a row each read 16 bytes next to one another.
+namespace kv4 {
+constexpr int PAGE = 64, GROUP = 32;
+__host__ __device__ constexpr int code_bytes(int hd) { return PAGE * hd / 2; }
+__host__ __device__ constexpr int record_bytes(int hd) { return PAGE * (hd / 2 + hd / GROUP * 4); }
+__host__ __device__ constexpr int word_at(int place, int w) { return (w / 4 * PAGE + place) * 16 + w % 4 * 4; }      // of dimensions 8 w .. 8 w + 7
+constexpr float LARGEST = 8.507059173023462e37f;      // 2^126: twice that, and a base 16 scales away, are still finite
+
+// Four pairs of values (dimensions 8 w .. 8 w + 7) of word `w`; ss = (s, s), bb = (b, b).
+__device__ __forceinline__ uint32_t pair_of(uint32_t shifted, uint32_t ss, uint32_t bb) {
+  const uint32_t v = (shifted & 0x00780078u) | 0x41804180u;
+  uint32_t r;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(ss), "r"(bb));
+  return r;
+}
+__device__ __forceinline__ void values8(uint32_t w, uint32_t ss, uint32_t bb, uint32_t (&out)[4]) {
+  out[0] = pair_of(w << 3, ss, bb); out[1] = pair_of(w >> 1, ss, bb); out[2] = pair_of(w >> 5, ss, bb); out[3] = pair_of(w >> 9, ss, bb);
+}
+__device__ __forceinline__ uint32_t low_twice(uint32_t sb) { return __byte_perm(sb, 0, 0x1010); }
+__device__ __forceinline__ uint32_t high_twice(uint32_t sb) { return __byte_perm(sb, 0, 0x3232); }
+}  // namespace kv4
+
+// Rows of K and V to the slots (64 page + place) that the page map gave them; a slot outside the pool is skipped.  Four threads share a group of 32
+// dimensions, eight each; a thread takes the same place of K and V, so that two loads are on their way at once.  What bounds it: memory, 2.5 bytes an element.
+__global__ void __launch_bounds__(256) kv4_store_kernel(const bf16 *__restrict__ k, long long k_stride, const bf16 *__restrict__ v, long long v_stride, const int32_t *__restrict__ slots,
+                                                        int n_rows, int heads, int hd, uint8_t *__restrict__ k_pages, uint8_t *__restrict__ v_pages, int n_pages) {
+  const int per_head = hd / 8, per_row = heads * per_head;              // threads (a multiple of eight: the four of a group lie in one warp)
+  const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  const long long row = i / per_row;
+  const int at = (int)(i - row * per_row), head = at / per_head, part = at % per_head;
+  const int slot = row < n_rows ? slots[row] : -1;
+  const bool live = slot >= 0 && slot / kv4::PAGE < n_pages;
+  uint4 raw[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+  if (live) {
+    raw[0] = *reinterpret_cast<const uint4 *>(k + row * k_stride + at * 8);
+    raw[1] = *reinterpret_cast<const uint4 *>(v + row * v_stride + at * 8);
+  }
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float x[8];
+    const __nv_bfloat162 *p = reinterpret_cast<const __nv_bfloat162 *>(&raw[which]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { const float2 f = __bfloat1622float2(p[e]); x[2 * e] = f.x; x[2 * e + 1] = f.y; }
+    float lo = 3e38f, hi = -3e38f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = x[e] != x[e] ? 0.f : fminf(fmaxf(x[e], -kv4::LARGEST), kv4::LARGEST);         // what is held is finite
+      lo = fminf(lo, x[e]); hi = fmaxf(hi, x[e]);
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) { lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o)); hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o)); }
+    const bf16 s16 = __float2bfloat16_rn(__fdiv_rn(hi - lo, 15.f));
+    const float s = __bfloat162float(s16);
+    const bf16 b16 = __float2bfloat16_rn(lo - 16.f * s);
+    const float b = __bfloat162float(b16);
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float c = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(x[e] - b, s)) - 16.f, 0.f), 15.f) : 0.f;
+      w |= (uint32_t)c << (4 * (e / 2) + 16 * (e % 2));
+    }
+    if (live) {
+      uint8_t *rec = (which ? v_pages : k_pages) + ((size_t)(slot / kv4::PAGE) * heads + head) * kv4::record_bytes(hd);
+      const int place = slot % kv4::PAGE;
+      *reinterpret_cast<uint32_t *>(rec + kv4::word_at(place, part)) = w;
+      if (part % 4 == 0)
+        *reinterpret_cast<uint32_t *>(rec + kv4::code_bytes(hd) + (place * (hd / kv4::GROUP) + part / 4) * 4) =
+            (uint32_t)__bfloat16_as_ushort(s16) | (uint32_t)__bfloat16_as_ushort(b16) << 16;
+    }
+  }
+}
+
+// The values at the listed slots as rows of K and V; a row whose slot is outside the pool is left as it is.
+__global__ void __launch_bounds__(256) kv4_load_kernel(const uint8_t *__restrict__ k_pages, const uint8_t *__restrict__ v_pages, int n_pages, const int32_t *__restrict__ slots, int n_rows,
+                                                       int heads, int hd, bf16 *__restrict__ k, long long k_stride, bf16 *__restrict__ v, long long v_stride) {
+  const int per_head = hd / 8, per_row = heads * per_head;
+  const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  const long long row = i / per_row;
+  if (row >= n_rows) return;
+  const int at = (int)(i - row * per_row), head = at / per_head, part = at % per_head;
+  const int slot = slots[row];
+  if (slot < 0 || slot / kv4::PAGE >= n_pages) return;
+  const size_t rec = ((size_t)(slot / kv4::PAGE) * heads + head) * kv4::record_bytes(hd);
+  const size_t code = rec + kv4::word_at(slot % kv4::PAGE, part), pair = rec + kv4::code_bytes(hd) + (slot % kv4::PAGE * (hd / kv4::GROUP) + part / 4) * 4;
+  const uint32_t wk = *reinterpret_cast<const uint32_t *>(k_pages + code), wv = *reinterpret_cast<const uint32_t *>(v_pages + code);
+  const uint32_t pk = *reinterpret_cast<const uint32_t *>(k_pages + pair), pv = *reinterpret_cast<const uint32_t *>(v_pages + pair);
+  uint32_t o[4];
+  kv4::values8(wk, kv4::low_twice(pk), kv4::high_twice(pk), o);
+  *reinterpret_cast<uint4 *>(k + row * k_stride + at * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+  kv4::values8(wv, kv4::low_twice(pv), kv4::high_twice(pv), o);
+  *reinterpret_cast<uint4 *>(v + row * v_stride + at * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// ---- page map ------------------------------------------------------------------------------
+struct PageMapArgs {
+  int n_seqs, n_free, width, max_rows;
+  const int32_t *seq_len, *n_new, *held, *free_pages, *free_begin;    // (free_begin may be null: 0)
+  int32_t *table, *held_out, *row_start, *slots, *counts;
+  int32_t *scratch;                     // [2], zero between calls: CTAs that are done, rows without a slot
+};
+constexpr int MAP_THREADS = 512, MAP_ROWS = 2048, MAP_MAX_SEQS = 4096;
+
+// Every CTA works out all sequences' first row and first fresh page (one scan over the lengths: cheaper than a second kernel that waits for the
+// first) and then fills its share of the slots and of the table.  The table entries that a sequence holds are only read and the ones behind them
+// only written, a fresh page is taken from the free list wherever it is needed, so the CTAs need nothing from one another; what may be
+// overwritten in place (held, the counters) is written by the CTA that finishes last.  Sums saturate.
+// Bound by latency: two dependent loads, a scan, a search.
+__global__ void __launch_bounds__(MAP_THREADS) page_map_kernel(const PageMapArgs a) {
+  extern __shared__ int32_t map_smem[];
+  int32_t *first_row = map_smem, *first_page = map_smem + a.n_seqs + 1;       // [n_seqs + 1] each
+  __shared__ int warp_rows[MAP_THREADS / 32], warp_pages[MAP_THREADS / 32];
+  __shared__ int missing, last;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  auto plus = [](int x, int y) { return (int)min((unsigned)x + (unsigned)y, 0x7fffffffu); };
+  struct Seq { int n, m, held, want; };
+  auto seq_of = [&](int i) {
+    Seq s;
+    s.n = a.seq_len[i];
+    s.m = s.n < 0 ? 0 : max(a.n_new[i], 0);
+    s.held = min(max(a.held[i], 0), a.width);
+    s.want = s.n < 0 ? 0 : (int)min(((long long)s.n + s.m + 63) / 64, (long long)a.width);
+    return s;
+  };
+  const int per = (a.n_seqs + MAP_THREADS - 1) / MAP_THREADS, i0 = min(tid * per, a.n_seqs), i1 = min(i0 + per, a.n_seqs);
+  int rows = 0, pages = 0;
+  for (int i = i0; i < i1; ++i) { const Seq s = seq_of(i); rows = plus(rows, s.m); pages = plus(pages, max(s.want - s.held, 0)); }
+  int sum_rows = rows, sum_pages = pages;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, sum_rows, o), y = __shfl_up_sync(0xffffffffu, sum_pages, o);
+    if (lane >= o) { sum_rows = plus(sum_rows, x); sum_pages = plus(sum_pages, y); }
+  }
+  if (lane == 31) { warp_rows[warp] = sum_rows; warp_pages[warp] = sum_pages; }
+  if (tid == 0) missing = 0;
+  __syncthreads();
+  int at_row = __shfl_up_sync(0xffffffffu, sum_rows, 1), at_page = __shfl_up_sync(0xffffffffu, sum_pages, 1);
+  if (lane == 0) at_row = at_page = 0;
+  for (int w = 0; w < warp; ++w) { at_row = plus(at_row, warp_rows[w]); at_page = plus(at_page, warp_pages[w]); }
+  const int begin = a.free_begin ? max(*a.free_begin, 0) : 0;
+  at_page = plus(at_page, begin);
+  for (int i = i0; i < i1; ++i) {
+    const Seq s = seq_of(i);
+    first_row[i] = at_row; first_page[i] = at_page;
+    at_row = plus(at_row, s.m); at_page = plus(at_page, max(s.want - s.held, 0));
+  }
+  if (i0 < i1 && i1 == a.n_seqs) { first_row[a.n_seqs] = at_row; first_page[a.n_seqs] = at_page; }
+  __syncthreads();
+  const int total = first_row[a.n_seqs];
+  auto fresh = [&](int at) { return at < a.n_free ? a.free_pages[at] : -1; };        // (saturated sums lie behind any list)
+  // table entries: a warp per sequence
+  for (int i = blockIdx.x * (MAP_THREADS / 32) + warp; i < a.n_seqs; i += gridDim.x * (MAP_THREADS / 32)) {
+    const Seq s = seq_of(i);
+    for (int e = s.held + lane; e < s.want; e += 32) a.table[(size_t)i * a.width + e] = fresh(plus(first_page[i], e - s.held));
+    if (lane == 0) a.row_start[i] = first_row[i];
+  }
+  // slots
+  int none = 0;
+  for (int r = blockIdx.x * MAP_ROWS + tid; r < min((blockIdx.x + 1) * MAP_ROWS, a.max_rows); r += MAP_THREADS) {
+    int slot = -1;
+    if (r < total) {
+      int lo = 0, hi = a.n_seqs;                       // the last sequence whose first row is at most r
+      while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (first_row[mid] <= r) lo = mid; else hi = mid; }
+      const long long pos = (long long)a.seq_len[lo] + (r - first_row[lo]);
+      const int held = min(max(a.held[lo], 0), a.width);
+      if (pos < (long long)a.width * 64) {
+        const int e = (int)(pos >> 6);
+        const int page = e < held ? a.table[(size_t)lo * a.width + e] : fresh(plus(first_page[lo], e - held));
+        if (page >= 0 && page < (1 << 25)) slot = page * 64 + (int)(pos & 63);
+      }
+      none += slot < 0;
+    }
+    a.slots[r] = slot;
+  }
+  none = __reduce_add_sync(0xffffffffu, none);
+  if (lane == 0 && none) atomicAdd(&missing, none);
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) {
+    if (missing) atomicAdd(&a.scratch[1], missing);
+    __threadfence();
+    last = atomicAdd(&a.scratch[0], 1) == (int)gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  // every CTA has read what may be overwritten in place
+  for (int i = tid; i < a.n_seqs; i += MAP_THREADS) { const Seq s = seq_of(i); a.held_out[i] = max(s.held, s.want); }
+  if (tid == 0) {
+    __threadfence();
+    const int without = *reinterpret_cast<volatile int32_t *>(&a.scratch[1]);
+    a.row_start[a.n_seqs] = total;
+    a.counts[0] = first_page[a.n_seqs];
+    a.counts[1] = plus(without, max(total - a.max_rows, 0));
+    a.counts[2] = total;
+    a.scratch[0] = 0; a.scratch[1] = 0;
+  }
+}
+
+// ---- what a row of a windowed call sees -----------------------------------------------------
+// The slots of a step (blocks = 1: k causal slots, then k blocks of k mask slots) or k causal slots alone.  A row sees the cached positions t < nvis with
+// t < sinks or t >= low, and local rows [loc0, loc0 + nloc).  Its sequence is absent (seq_len < 0): n < 0.
+struct WindowRows {
+  const int32_t *seq_len; int k, blocks, n_max, window, sinks;
+  __host__ __device__ int rows() const { return blocks ? k * (k + 1) : k; }
+};
+struct WindowKeys { int n, nvis, low, loc0, nloc, seq; };
+__device__ __forceinline__ WindowKeys window_keys(const WindowRows &w, int r) {
+  const int T = w.rows(), s = r / T, slot = r - s * T;
+  WindowKeys o{};
+  o.seq = s;
+  o.n = min(w.seq_len[s], w.n_max);
+  if (o.n < 0) return o;
+  int pos;
+  if (slot < w.k) { o.nvis = o.n + slot + 1; pos = o.n + slot; }
+  else {
+    const int b = (slot - w.k) / w.k;
+    o.nvis = o.n + b + 1; o.loc0 = s * w.k * w.k + b * w.k; o.nloc = w.k;
+    pos = o.n + b + 1 + (slot - w.k - b * w.k);
+  }
+  o.low = w.window > 0 ? max(pos - w.window + 1, 0) : 0;
+  return o;
+}
+
+// What the attention kernels over a caller's pages are given.
+struct CacheArgs {
+  const bf16 *q; long long q_stride;
+  const void *k_pages, *v_pages; int n_pages;
+  const int32_t *table; int width;
+  const bf16 *k_local, *v_local; long long local_stride;
+  bf16 *out;
+  int Hq, Hkv;
+  WindowRows rows;
+};
+
+// One warp per (row, query head), 32 keys at a time, fp32 throughout.
+template <int HD, bool KV4>
+__global__ void __launch_bounds__(32) attn_cache_replay_kernel(const CacheArgs a, float scale) {
+  constexpr int DPL = HD / 32;
+  __shared__ float qs[HD];
+  __shared__ float vs[32][HD + 1];
+  const int r = blockIdx.x, h = blockIdx.y, lane = threadIdx.x, kvh = h / (a.Hq / a.Hkv);
+  const WindowKeys w = window_keys(a.rows, r);
+  if (w.n < 0) return;
+  const bf16 *q = a.q + r * a.q_stride + h * HD;
+  for (int c = lane; c < HD; c += 32) qs[c] = __bfloat162float(q[c]) * scale;
+  __syncwarp();
+  float mx = -INFINITY, den = 0.f, acc[DPL] = {};
+  // keys in the order: sinks, window, local rows
+  const int n_sink = min(a.rows.window > 0 ? a.rows.sinks : 0, w.nvis), low = max(w.low, n_sink), n_window = max(w.nvis - low, 0), total = n_sink + n_window + w.nloc;
+  for (int t0 = 0; t0 < total; t0 += 32) {
+    const int t = t0 + lane;
+    float sc = -INFINITY;
+    bool live = false;
+    auto row_of = [&](const bf16 *k, const bf16 *v) {
+      float dot = 0.f;
+      for (int c = 0; c < HD; ++c) { dot = fmaf(__bfloat162float(k[c]), qs[c], dot); vs[lane][c] = __bfloat162float(v[c]); }
+      sc = dot; live = true;
+    };
+    if (t < n_sink + n_window) {
+      const int pos = t < n_sink ? t : low + (t - n_sink);
+      const int page = a.table[(size_t)w.seq * a.width + pos / 64];
+      if ((unsigned)page < (unsigned)a.n_pages) {        // (a page outside the pool is seen by no row)
+        const size_t head = (size_t)page * a.Hkv + kvh;
+        if constexpr (KV4) {
+          const uint8_t *kr = (const uint8_t *)a.k_pages + head * kv4::record_bytes(HD), *vr = (const uint8_t *)a.v_pages + head * kv4::record_bytes(HD);
+          float dot = 0.f;
+          for (int c = 0; c < HD; c += 8) {
+            const int code = kv4::word_at(pos % 64, c / 8), pair = kv4::code_bytes(HD) + (pos % 64 * (HD / 32) + c / 32) * 4;
+            const uint32_t kp = *reinterpret_cast<const uint32_t *>(kr + pair), vp = *reinterpret_cast<const uint32_t *>(vr + pair);
+            uint32_t x[4], y[4];
+            kv4::values8(*reinterpret_cast<const uint32_t *>(kr + code), kv4::low_twice(kp), kv4::high_twice(kp), x);
+            kv4::values8(*reinterpret_cast<const uint32_t *>(vr + code), kv4::low_twice(vp), kv4::high_twice(vp), y);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 f = __bfloat1622float2(*reinterpret_cast<__nv_bfloat162 *>(&x[e])), g = __bfloat1622float2(*reinterpret_cast<__nv_bfloat162 *>(&y[e]));
+              dot = fmaf(f.x, qs[c + 2 * e], dot); dot = fmaf(f.y, qs[c + 2 * e + 1], dot);
+              vs[lane][c + 2 * e] = g.x; vs[lane][c + 2 * e + 1] = g.y;
+            }
+          }
+          sc = dot; live = true;
+        } else {
+          row_of((const bf16 *)a.k_pages + (head * 64 + pos % 64) * HD, (const bf16 *)a.v_pages + (head * 64 + pos % 64) * HD);
+        }
+      }
+    } else if (t < total) {
+      const long long at = (w.loc0 + (t - n_sink - n_window)) * a.local_stride + kvh * HD;
+      row_of(a.k_local + at, a.v_local + at);
+    }
+    const float top = fmaxf(mx, warp_max(sc));
+    const float keep = top == -INFINITY ? 1.f : __expf(mx - top);
+    const float p = live ? __expf(sc - top) : 0.f;
+    den = den * keep + warp_sum(p);
+#pragma unroll
+    for (int i = 0; i < DPL; ++i) acc[i] *= keep;
+    mx = top;
+    const unsigned seen = __ballot_sync(0xffffffffu, live);
+    for (int j = 0; j < 32; ++j) {
+      const float pj = __shfl_sync(0xffffffffu, p, j);
+      if (!(seen >> j & 1)) continue;
+#pragma unroll
+      for (int i = 0; i < DPL; ++i) acc[i] = fmaf(pj, vs[j][lane + 32 * i], acc[i]);
+    }
+    __syncwarp();
+  }
+  bf16 *o = a.out + ((size_t)r * a.Hq + h) * HD;
+#pragma unroll
+  for (int i = 0; i < DPL; ++i) o[lane + 32 * i] = __float2bfloat16(den > 0.f ? acc[i] / den : 0.f);      // no visible key: zeros
+}

@@ -15,6 +15,7 @@
 #include "kernels_replay.cuh"
 #include "gemm_tc.cuh"
 #include "attn_tc.cuh"
+#include "kernels_cache.cuh"
 
 namespace {
 
@@ -119,6 +120,8 @@ struct tidar_ctx {
   int64_t graphs_captured = 0, graphs_launched = 0;
   bool slab_bf16 = false;          // split-K partial sums of the step in bf16 instead of fp32 (config debug bit 2)
   int32_t *d_status = nullptr, *cand_idx = nullptr;
+  int32_t *d_map = nullptr;        // page map: see PageMapArgs::scratch
+  static constexpr int MAP_INTS = 64;
   float *cand_val = nullptr;
   // in-kernel timeline (diagnostics): two words per launch of the last recorded step
   static constexpr int TL_MAX = 2048;
@@ -218,6 +221,7 @@ void layout(tidar_ctx &x, void *arena, size_t *bytes) {
   x.d_prompt = cv.take<int32_t>(c.max_seq_len);
   x.d_arg_idx = cv.take<int32_t>(R); x.d_arg_val = cv.take<float>(R);
   x.d_status = cv.take<int32_t>(64);
+  x.d_map = cv.take<int32_t>(tidar_ctx::MAP_INTS);
   x.d_tl = cv.take<unsigned long long>(2 * tidar_ctx::TL_MAX + 8);   // timeline slots, then diagnostic counters
   if (c.impl == 0) {
     const size_t slots = (size_t)attn_tc::SLOTS_PER_SM * MAX_SMS;
@@ -1423,6 +1427,7 @@ int tidar_init(const tidar_config *cfg, const tidar_weights *w, void *arena, siz
   }
   e = cudaMemsetAsync(c->d_seq_len, 0, cfg->max_batch * sizeof(int), c->stream);
   if (e == cudaSuccess) e = cudaMemsetAsync(c->d_status, 0, 64 * sizeof(int), c->stream);
+  if (e == cudaSuccess) e = cudaMemsetAsync(c->d_map, 0, tidar_ctx::MAP_INTS * sizeof(int), c->stream);
   if (e == cudaSuccess) e = cudaMemsetAsync(c->d_page_table, 0, (size_t)cfg->max_batch * c->pages_per_seq * sizeof(int), c->stream);
   if (e == cudaSuccess) e = cudaStreamSynchronize(c->stream);
   if (e != cudaSuccess) { cudaFreeHost(c->h_pinned); delete c; return fail(nullptr, TIDAR_ECUDA, "arena set-up: %s", cudaGetErrorString(e)); }
@@ -1915,6 +1920,112 @@ int tidar_attention(tidar_ctx *c, const void *q, const void *k_pages, const void
   CUDA_TRY(c, cudaGetLastError());
   return TIDAR_OK;
 }
+
+// ---- a paged cache that the caller keeps ----
+int tidar_kv4_page_bytes(int32_t head_dim, size_t *out_bytes) {
+  if (!out_bytes) return fail(nullptr, TIDAR_EINVAL, "null argument");
+  if (head_dim != 64 && head_dim != 128) return fail(nullptr, TIDAR_EINVAL, "head_dim must be 64 or 128");
+  *out_bytes = (size_t)kv4::record_bytes(head_dim);
+  return TIDAR_OK;
+}
+
+int tidar_page_map(tidar_ctx *c, const int32_t *seq_len, const int32_t *n_new, const int32_t *held, int32_t n_seqs, const int32_t *free_pages, int32_t n_free,
+                   const int32_t *free_begin, int32_t *page_table, int32_t pages_per_seq, int32_t *held_out, int32_t *row_start, int32_t *slots, int32_t max_rows, int32_t *counts) {
+  if (!c) return TIDAR_EINVAL;
+  if (!seq_len || !n_new || !held || !page_table || !held_out || !row_start || !counts || (!free_pages && n_free > 0) || (!slots && max_rows > 0)) return fail(c, TIDAR_EINVAL, "null argument");
+  if (((uintptr_t)seq_len | (uintptr_t)n_new | (uintptr_t)held | (uintptr_t)free_pages | (uintptr_t)free_begin | (uintptr_t)page_table | (uintptr_t)held_out | (uintptr_t)row_start |
+       (uintptr_t)slots | (uintptr_t)counts) % 4)
+    return fail(c, TIDAR_EINVAL, "arrays must be 4-byte aligned");
+  if (n_seqs < 1 || n_seqs > MAP_MAX_SEQS) return fail(c, TIDAR_EINVAL, "n_seqs must be in [1, %d]", MAP_MAX_SEQS);
+  if (n_free < 0 || max_rows < 0 || max_rows > INT32_MAX - MAP_ROWS) return fail(c, TIDAR_EINVAL, "n_free and max_rows must not be negative, nor max_rows above 2^31 - 2049");
+  if (pages_per_seq < 1 || pages_per_seq > (1 << 25) - 1) return fail(c, TIDAR_EINVAL, "pages_per_seq must be in [1, 2^25 - 1]");
+  if (!c->inflight.empty()) return fail(c, TIDAR_EINVAL, "a step is in flight");
+  const PageMapArgs a{n_seqs, n_free, pages_per_seq, max_rows, seq_len, n_new, held, free_pages, free_begin, page_table, held_out, row_start, slots, counts, c->d_map};
+  const int grid = std::max((max_rows + MAP_ROWS - 1) / MAP_ROWS, 1);
+  {
+    Launch l(c, TIDAR_TC_EMBED);
+    page_map_kernel<<<grid, MAP_THREADS, 2 * (n_seqs + 1) * sizeof(int32_t), c->stream>>>(a);
+  }
+  CUDA_TRY(c, cudaGetLastError());
+  return TIDAR_OK;
+}
+
+static int check_kv4_rows(tidar_ctx *c, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *slots, int32_t n_rows, const void *k_pages, const void *v_pages, int32_t n_pages) {
+  if (!c) return TIDAR_EINVAL;
+  if (!k || !v || !slots || !k_pages || !v_pages) return fail(c, TIDAR_EINVAL, "null argument");
+  if (n_rows < 0 || n_pages < 1 || n_pages >= (1 << 25)) return fail(c, TIDAR_EINVAL, "n_rows must not be negative, n_pages in [1, 2^25)");
+  const int row = c->cfg.n_kv_heads * c->cfg.head_dim;
+  if (k_stride < row || v_stride < row || k_stride % 8 || v_stride % 8) return fail(c, TIDAR_EINVAL, "row strides must be multiples of 8 elements and hold n_kv_heads * head_dim of them");
+  if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)k_pages | (uintptr_t)v_pages) % 16 || (uintptr_t)slots % 4) return fail(c, TIDAR_EINVAL, "tensors must be 16-byte aligned (slots 4-byte)");
+  if ((long long)n_rows * (row / 8) > (long long)INT32_MAX * 256) return fail(c, TIDAR_EINVAL, "too many rows for one call");
+  if (!c->inflight.empty()) return fail(c, TIDAR_EINVAL, "a step is in flight");
+  return TIDAR_OK;
+}
+
+int tidar_kv4_store(tidar_ctx *c, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *slots, int32_t n_rows, void *k_pages, void *v_pages, int32_t n_pages) {
+  if (int rc = check_kv4_rows(c, k, k_stride, v, v_stride, slots, n_rows, k_pages, v_pages, n_pages)) return rc;
+  const tidar_config &cf = c->cfg;
+  const long long threads = (long long)n_rows * cf.n_kv_heads * cf.head_dim / 8;
+  if (threads) {
+    Launch l(c, TIDAR_TC_ROPE);
+    kv4_store_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, c->stream>>>((const bf16 *)k, k_stride, (const bf16 *)v, v_stride, slots, n_rows, cf.n_kv_heads, cf.head_dim,
+                                                                             (uint8_t *)k_pages, (uint8_t *)v_pages, n_pages);
+  }
+  CUDA_TRY(c, cudaGetLastError());
+  return TIDAR_OK;
+}
+
+int tidar_kv4_load(tidar_ctx *c, const void *k_pages, const void *v_pages, int32_t n_pages, const int32_t *slots, int32_t n_rows, void *k, int64_t k_stride, void *v, int64_t v_stride) {
+  if (int rc = check_kv4_rows(c, k, k_stride, v, v_stride, slots, n_rows, k_pages, v_pages, n_pages)) return rc;
+  const tidar_config &cf = c->cfg;
+  const long long threads = (long long)n_rows * cf.n_kv_heads * cf.head_dim / 8;
+  if (threads) {
+    Launch l(c, TIDAR_TC_ROPE);
+    kv4_load_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, c->stream>>>((const uint8_t *)k_pages, (const uint8_t *)v_pages, n_pages, slots, n_rows, cf.n_kv_heads, cf.head_dim,
+                                                                            (bf16 *)k, k_stride, (bf16 *)v, v_stride);
+  }
+  CUDA_TRY(c, cudaGetLastError());
+  return TIDAR_OK;
+}
+
+static int attention_over_cache(tidar_ctx *c, const tidar_attention_args *x, bool four_bits) {
+  if (!c) return TIDAR_EINVAL;
+  if (!x || !x->q || !x->k_pages || !x->v_pages || !x->page_table || !x->seq_len || !x->out) return fail(c, TIDAR_EINVAL, "null argument");
+  if (!x->k_local != !x->v_local) return fail(c, TIDAR_EINVAL, "k_local and v_local come together or not at all");
+  const tidar_config &cf = c->cfg;
+  const int blocks = x->k_local ? 1 : 0;
+  if (x->k < 1 || (blocks && x->k > cf.k_max)) return fail(c, TIDAR_EINVAL, "k must be positive, and at most k_max where there are mask blocks");
+  const long long R = (long long)std::max(x->n_seqs, 0) * x->k * (blocks ? x->k + 1 : 1);
+  if (x->n_seqs < 1 || R > c->R_cap) return fail(c, TIDAR_EINVAL, "%lld rows; the context has room for %d (max_batch, k_max, prefill_rows)", R, c->R_cap);
+  if (x->n_pages < 1 || x->n_pages >= (1 << 25) || x->pages_per_seq < 1 || x->pages_per_seq >= (1 << 25)) return fail(c, TIDAR_EINVAL, "n_pages and pages_per_seq must be in [1, 2^25)");
+  if ((long long)x->pages_per_seq * 64 < x->k) return fail(c, TIDAR_EINVAL, "the page table cannot back the k causal slots");
+  if (x->window < 0 || x->sinks < 0) return fail(c, TIDAR_EINVAL, "window and sinks must not be negative");
+  const int q_row = cf.n_q_heads * cf.head_dim, kv_row = cf.n_kv_heads * cf.head_dim;
+  const long long q_stride = x->q_stride ? x->q_stride : q_row, local_stride = x->local_stride ? x->local_stride : kv_row;
+  if (q_stride < q_row || q_stride % 8 || local_stride < kv_row || local_stride % 8 || q_stride > (1 << 30) || local_stride > (1 << 30))
+    return fail(c, TIDAR_EINVAL, "row strides must be multiples of 8 elements, hold a row, and be at most 2^30");
+  if (((uintptr_t)x->q | (uintptr_t)x->k_pages | (uintptr_t)x->v_pages | (uintptr_t)x->k_local | (uintptr_t)x->v_local | (uintptr_t)x->out) % 16 ||
+      ((uintptr_t)x->page_table | (uintptr_t)x->seq_len) % 4)
+    return fail(c, TIDAR_EINVAL, "tensors must be 16-byte aligned (page_table and seq_len 4-byte)");
+  if (!c->inflight.empty()) return fail(c, TIDAR_EINVAL, "a step is in flight");
+  CacheArgs a{(const bf16 *)x->q, q_stride, x->k_pages, x->v_pages, x->n_pages, x->page_table, x->pages_per_seq, (const bf16 *)x->k_local, (const bf16 *)x->v_local, local_stride,
+              (bf16 *)x->out, cf.n_q_heads, cf.n_kv_heads, WindowRows{x->seq_len, x->k, blocks, x->pages_per_seq * 64 - x->k, x->window, x->sinks}};
+  {
+    Launch l(c, TIDAR_TC_ATTN);
+    const dim3 grid((unsigned)R, cf.n_q_heads);
+    const float scale = 1.0f / sqrtf((float)cf.head_dim);
+    if (cf.head_dim == 128) {
+      if (four_bits) attn_cache_replay_kernel<128, true><<<grid, 32, 0, c->stream>>>(a, scale); else attn_cache_replay_kernel<128, false><<<grid, 32, 0, c->stream>>>(a, scale);
+    } else {
+      if (four_bits) attn_cache_replay_kernel<64, true><<<grid, 32, 0, c->stream>>>(a, scale); else attn_cache_replay_kernel<64, false><<<grid, 32, 0, c->stream>>>(a, scale);
+    }
+  }
+  CUDA_TRY(c, cudaGetLastError());
+  return TIDAR_OK;
+}
+
+int tidar_attention_kv4(tidar_ctx *c, const tidar_attention_args *args) { return attention_over_cache(c, args, true); }
+int tidar_attention_window(tidar_ctx *c, const tidar_attention_args *args) { return attention_over_cache(c, args, false); }
 
 }  // extern "C"
 

@@ -1,0 +1,78 @@
+"""Host-side checks of the operators over a caller's paged cache (no GPU needed)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from tests import cache_helpers as H
+from paper_2511_08923_b200 import Tidar, TidarError, binding, kv4_page_bytes
+
+
+def test_page_bytes():
+    assert kv4_page_bytes(64) == 64 * (32 + 8) and kv4_page_bytes(128) == 64 * (64 + 16)
+    for hd in (0, 32, 96, 256, -64):
+        with pytest.raises(TidarError):
+            kv4_page_bytes(hd)
+    assert binding.load().tidar_kv4_page_bytes(64, None) == -1
+
+
+def test_calls_without_a_context_are_refused():
+    lib = binding.load()
+    assert lib.tidar_page_map(None, *[None] * 3, 1, None, 0, None, None, 1, None, None, None, 0, None) == -1
+    assert lib.tidar_kv4_store(None, None, 8, None, 8, None, 0, None, None, 1) == -1
+    assert lib.tidar_kv4_load(None, None, None, 1, None, 0, None, 8, None, 8) == -1
+    assert lib.tidar_attention_kv4(None, None) == -1 and lib.tidar_attention_window(None, None) == -1
+
+
+def test_the_binding_refuses_tensors_of_another_device_type_or_shape():
+    t = Tidar.__new__(Tidar)
+    t.device = torch.device("cuda:0")
+    for x in (torch.zeros(3), None, [1, 2]):
+        with pytest.raises(ValueError):
+            t._tensor("x", x, torch.float32, (3,))
+
+
+def test_argument_struct_is_laid_out_as_in_c(tmp_path):
+    """Offsets of tidar_attention_args as the C compiler has them."""
+    import os
+    import shutil
+    import subprocess
+    cc = shutil.which("gcc") or shutil.which("cc")
+    if cc is None:
+        pytest.skip("no C compiler")
+    names = [n for n, _ in binding.tidar_attention_args._fields_]
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "o.c"
+    src.write_text('#include <stdio.h>\n#include "tidar.h"\nint main(void) {\n' + "".join(f'printf("%zu ", offsetof(tidar_attention_args, {n}));\n' for n in names) +
+                   'printf("%zu", sizeof(tidar_attention_args)); return 0; }\n')
+    subprocess.run([cc, "-I", os.path.join(root, "include"), str(src), "-o", str(tmp_path / "o")], check=True)
+    got = [int(x) for x in subprocess.run([str(tmp_path / "o")], capture_output=True, text=True, check=True).stdout.split()]
+    assert got == [getattr(binding.tidar_attention_args, n).offset for n in names] + [C.sizeof(binding.tidar_attention_args)]
+
+
+def test_the_plain_statement_of_4_bit_rows():
+    """Codes come back as the values that the definition names, and those are within a step of what was stored."""
+    rng = np.random.default_rng(1)
+    x = H.bf16_round(rng.standard_normal((3, 64, 128)) * 3)
+    c, s, b = H.quantise(x)
+    assert c.min() >= 0 and c.max() <= 15
+    y = H.values(c, s, b)
+    assert (np.abs(y - x) <= np.repeat(s, 32, -1) * 0.75 + 2.0 ** -8 * np.abs(x)).all()
+    rec = H.records(x)
+    assert rec.shape == (3, kv4_page_bytes(128))
+    word = rec[0, :4].astype(np.uint32)
+    word = word[0] | word[1] << 8 | word[2] << 16 | word[3] << 24
+    assert [int(word >> (4 * (d // 2) + 16 * (d % 2)) & 15) for d in range(8)] == c[0, 0, :8].tolist()
+    # how readers get from codes to values: 16 + c is the bf16 number with the code in its upper mantissa bits
+    for code in range(16):
+        assert np.array([0x4180 | code << 3], dtype=np.uint32).__lshift__(16).view(np.float32)[0] == 16 + code
+
+
+def test_visibility_by_cases():
+    v = H.visible(10, 2, True, 4, 3, 12)
+    assert np.nonzero(v[0])[0].tolist() == [0, 1, 2, 7, 8, 9, 10]           # causal slot 0, position 10
+    assert np.nonzero(v[1])[0].tolist() == [0, 1, 2, 8, 9, 10, 11]
+    assert np.nonzero(v[2])[0].tolist() == [0, 1, 2, 8, 9, 10]              # block 0, slot 0: position 11
+    assert np.nonzero(v[5])[0].tolist() == [0, 1, 2, 10, 11]                # block 1, slot 1: position 13
+    assert H.visible(10, 2, True, 0, 0, 12)[5].sum() == 12
