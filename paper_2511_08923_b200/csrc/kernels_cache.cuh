@@ -1,5 +1,5 @@
 // A paged cache that the caller keeps: page map of a batch, K and V rows held in 4 bits, and the plain attention over such pages or bf16
-// pages with a sliding window.
+// pages with a sliding window.  (The kernel for few rows over 4-bit pages: attn_few.cuh.)
 #pragma once
 #include "common.cuh"
 
@@ -243,7 +243,7 @@ struct CacheArgs {
   WindowRows rows;
 };
 
-// One warp per (row, query head), 32 keys at a time, fp32 throughout.
+// One warp per (row, query head), 32 keys at a time, fp32 throughout (impl 1).
 template <int HD, bool KV4>
 __global__ void __launch_bounds__(32) attn_cache_replay_kernel(const CacheArgs a, float scale) {
   constexpr int DPL = HD / 32;

@@ -16,6 +16,7 @@
 #include "gemm_tc.cuh"
 #include "attn_tc.cuh"
 #include "kernels_cache.cuh"
+#include "attn_few.cuh"
 
 namespace {
 
@@ -120,8 +121,8 @@ struct tidar_ctx {
   int64_t graphs_captured = 0, graphs_launched = 0;
   bool slab_bf16 = false;          // split-K partial sums of the step in bf16 instead of fp32 (config debug bit 2)
   int32_t *d_status = nullptr, *cand_idx = nullptr;
-  int32_t *d_map = nullptr;        // page map: see PageMapArgs::scratch
-  static constexpr int MAP_INTS = 64;
+  int32_t *d_map = nullptr;        // page map: see PageMapArgs::scratch; from FEW_ARRIVED on, attn_few::Args::arrived
+  static constexpr int MAP_INTS = 1024, FEW_ARRIVED = 64;
   float *cand_val = nullptr;
   // in-kernel timeline (diagnostics): two words per launch of the last recorded step
   static constexpr int TL_MAX = 2048;
@@ -724,6 +725,23 @@ void launch_attention(tidar_ctx *c, const bf16 *Q, const bf16 *Kp, const bf16 *V
     attn_replay_kernel<64><<<grid, 32, 0, c->stream>>>(Q, Kp, Vp, g, c->meta, Kl, Vl, O, c->cfg.n_q_heads, scale);
 }
 
+// 4-bit pages: sequences of so few rows per KV head go through attn_few_kernel.
+bool few_rows(const tidar_ctx *c, const WindowRows &w) { return w.rows() * (c->cfg.n_q_heads / c->cfg.n_kv_heads) <= 2 * attn_few::ROWS; }
+
+void launch_few(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
+  Launch l(c, TIDAR_TC_ATTN);
+  attn_few::Args a{};
+  a.c = x; a.n_seqs = n_seqs;
+  a.tiles = (x.rows.rows() * (x.Hq / x.Hkv) + attn_few::ROWS - 1) / attn_few::ROWS;
+  a.ctas = attn_few::CTAS_PER_SM * c->n_sms; a.per_warp = 1;
+  a.scale_log2 = 1.4426950408889634f / sqrtf((float)c->cfg.head_dim);
+  a.part_O = c->attn_part_O; a.part_ml = c->attn_part_ml; a.arrived = c->d_map + tidar_ctx::FEW_ARRIVED;
+  static_assert(attn_few::CTAS_PER_SM * MAX_SMS * 2 * attn_few::ROWS <= attn_tc::SLOTS_PER_SM * MAX_SMS * 2 * 128 &&
+                tidar_ctx::FEW_ARRIVED + attn_few::CTAS_PER_SM * MAX_SMS <= tidar_ctx::MAP_INTS, "partial results and counters fit the scratch");
+  if (c->cfg.head_dim == 128) launch_pdl(attn_few::attn_few_kernel<128>, a.ctas, attn_few::WARPS * 32, attn_few::Smem<128>::TOTAL, c->stream, a);
+  else launch_pdl(attn_few::attn_few_kernel<64>, a.ctas, attn_few::WARPS * 32, attn_few::Smem<64>::TOTAL, c->stream, a);
+}
+
 // How the norm of R rows of d floats with S fp32 partial results each is launched.
 // Behind a projection of many rows the blocks would all crowd onto the SMs that run out of work first (5.6 instead of
 // 3.6 us at 272 rows); claiming a share of the shared memory spreads them evenly.  With few rows they must leave room
@@ -906,6 +924,8 @@ int init_tensor_core_path(tidar_ctx *c) {
     CUDA_TRY(c, cudaMemsetAsync(c->Kloc, 0, nloc * cf.n_kv_heads * cf.head_dim * sizeof(bf16), c->stream));
     CUDA_TRY(c, cudaMemsetAsync(c->Vloc, 0, nloc * cf.n_kv_heads * cf.head_dim * sizeof(bf16), c->stream));
     auto smem = [](const void *f, int bytes) { return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
+    CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<128>, attn_few::Smem<128>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<64>, attn_few::Smem<64>::TOTAL));
     CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 2, false, false, false>, attn_tc::Smem<128, 2>::TOTAL));
     CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 2, false, true, false>, attn_tc::Smem<128, 2>::TOTAL));
     CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<64, 2, false, false, false>, attn_tc::Smem<64, 2>::TOTAL));
@@ -2010,7 +2030,8 @@ static int attention_over_cache(tidar_ctx *c, const tidar_attention_args *x, boo
   if (!c->inflight.empty()) return fail(c, TIDAR_EINVAL, "a step is in flight");
   CacheArgs a{(const bf16 *)x->q, q_stride, x->k_pages, x->v_pages, x->n_pages, x->page_table, x->pages_per_seq, (const bf16 *)x->k_local, (const bf16 *)x->v_local, local_stride,
               (bf16 *)x->out, cf.n_q_heads, cf.n_kv_heads, WindowRows{x->seq_len, x->k, blocks, x->pages_per_seq * 64 - x->k, x->window, x->sinks}};
-  {
+  if (cf.impl == 0 && four_bits && few_rows(c, a.rows)) launch_few(c, a, x->n_seqs);
+  else {
     Launch l(c, TIDAR_TC_ATTN);
     const dim3 grid((unsigned)R, cf.n_q_heads);
     const float scale = 1.0f / sqrtf((float)cf.head_dim);
