@@ -46,15 +46,21 @@
 // Partial (max, sum, O) results of a tile with several items are merged by attn_combine_kernel.
 // A stand-alone call pays for its plan alone (4.5 us).  Where there is little to distribute it does without: every CTA
 // works out its own item (direct_item), with an instance of one stream per CTA where that saves a wave.
+//
+// Calls over a caller's pages with a sliding window, and over 4-bit pages, are instances of the same kernel (CACHE, see Window): what differs is which
+// pages an item has, what is masked, and how pages get to shared memory.
 #pragma once
 #include "common.cuh"
+#include "kernels_cache.cuh"
 #include "sm100_ptx.cuh"
 
 namespace attn_tc {
 
 constexpr int PAGE = 64;             // keys per step (= page size)
 // warp 0: K loads, 1: MMA, 2: watcher, 3: Q and V loads; warps 4..7 / 8..11: softmax of stream A / B
-__host__ __device__ constexpr int threads(int streams) { return 128 + 128 * streams; }
+// (KV4: and four more, which turn codes into operand tiles)
+enum { PLAIN = 0, WINDOW = 1, KV4 = 2 };       // CACHE: the library's pages and tidar_attention's; a caller's pages within a window, bf16; the same in 4 bits
+__host__ __device__ constexpr int threads(int streams, int cache = PLAIN) { return 128 + 128 * streams + (cache == KV4 ? 128 : 0); }
 constexpr int MAX_SPLITS = 32;       // items per tile
 constexpr int MAX_CLUSTER = 8;       // CTAs that may share an item
 constexpr int SLOTS_PER_SM = 2;      // partial results that fit the scratch = grid of a pass whose key ranges may be split
@@ -62,7 +68,8 @@ constexpr float RAISE_THRESHOLD = 8.f;   // log2 units
 
 // Pages [p_begin, p_end) of the query tile that covers slots [row0, min(row0 + spt, row_end)) of sequence slot `seq`
 // and, if pair, of the tile behind it.  Its keys in pages: n_cache_pages cached ones, then step-local rows from loc_lo on.
-struct __align__(16) Item { int32_t row0, row_end, seq, p_begin, p_end, n_cache_pages, loc_lo, pair, split, pad[3]; };
+// Within a window the cached pages are the sequence's first ones up to the sinks' last (Window::sink_pages) and those from `skip` behind them on.
+struct __align__(16) Item { int32_t row0, row_end, seq, p_begin, p_end, n_cache_pages, loc_lo, pair, split, skip, pad[2]; };
 // A query tile: its items are item0 .. item0 + n_items - 1 (n_items = 0: no rows); in a pair, sub says which half it is.
 struct __align__(16) Tile { int32_t row0, row_end, item0, n_items, sub, pad[3]; };
 
@@ -80,7 +87,16 @@ struct PlanArgs {
   int n_sms, max_items;     // items a pass may have; n_units = every unit is one item
   int max_pieces;           // items a tile or pair may have (1: nothing is split, the merge kernel is not launched)
   int singles;              // tiles are not paired (an item is shared by a cluster, see attn_tc_kernel)
+  int sink_pages;           // see Window
   Item *items; Tile *tiles; // out: [max_items] (unused ones are zero), [2 n_units] (only where items may be split)
+};
+
+// What a call over a caller's pages brings with it.
+struct Window {
+  WindowRows rows;
+  int sink_pages;           // pages that hold sinks (0 without a window): always among a tile's pages
+  int n_pages;              // pages outside [0, n_pages) are seen by no row
+  const uint8_t *k4, *v4;   // 4-bit records
 };
 
 struct Args {
@@ -101,6 +117,7 @@ struct Args {
   struct { const int32_t *seq_len; int k, n_max; int per_group, pieces; } direct;    // query tiles per sequence, items per tile at most
   int *status;
   unsigned long long *tile_count;            // diagnostics: += steps this CTA computes (null = off)
+  Window win;                                // CACHE instances
 };
 
 // Shared memory of one CTA; everything is dynamic so that the 1024-byte alignment the
@@ -191,10 +208,14 @@ __host__ __device__ inline float plan_time(const PlanCost &c, int Hkv, int n_sms
 
 // What a row sees: cached positions [0, nvis), local rows [loc0, loc0 + nloc).
 struct RowKeys { int nvis, loc0, nloc, seq; };
+// Cached pages behind the sinks' that no row sees whose window begins at position `low` or later.
+__device__ __forceinline__ int skipped_pages(int low, int n_cache, int sink_pages) { return max(min(low / PAGE, n_cache) - sink_pages, 0); }
+static_assert(sizeof(RowKeys) != sizeof(WindowKeys), "plan_block tells them apart by size");
 
 template <typename ROW>
 __device__ inline void plan_block(const PlanArgs &p, ROW row_keys) {
-  struct Keys { int n_cache, n_pages, loc_lo; };       // (a sequence of more than 32767 pages fits a B200)
+  constexpr bool WINDOWED = sizeof(row_keys(0)) == sizeof(WindowKeys);
+  struct Keys { int n_cache, n_pages, loc_lo, skip; }; // (a sequence of more than 32767 pages fits a B200)
   __shared__ Keys keys[3][PLAN_UNITS];                 // tile 0, tile 1, the unit
   __shared__ int unit_row0[PLAN_UNITS], unit_rend[PLAN_UNITS], unit_seq[PLAN_UNITS];
   __shared__ float ent_us[3 * PLAN_UNITS];             // units, then tiles
@@ -213,9 +234,10 @@ __device__ inline void plan_block(const PlanArgs &p, ROW row_keys) {
       row0 = grp * p.rows_per_group + i * 2 * p.spt;
       row_end = min((grp + 1) * p.rows_per_group, p.R);
     }
-    int nvis[2] = {0, 0}, lo[2] = {0x7fffffff, 0x7fffffff}, hi[2] = {0, 0}, seq = 0;
+    int nvis[2] = {0, 0}, lo[2] = {0x7fffffff, 0x7fffffff}, hi[2] = {0, 0}, seq = 0, low[2] = {0x7fffffff, 0x7fffffff};
     for (int r = row0 + lane; r < min(row0 + 2 * p.spt, row_end); r += 32) {
-      const RowKeys k = row_keys(r);
+      const auto k = row_keys(r);
+      if constexpr (WINDOWED) { if (k.nvis > 0) { if (r >= row0 + p.spt) low[1] = min(low[1], k.low); else low[0] = min(low[0], k.low); } }
       const int t = r >= row0 + p.spt;
       seq = k.seq;
       if (t) { nvis[1] = max(nvis[1], k.nvis); if (k.nloc > 0) { lo[1] = min(lo[1], k.loc0); hi[1] = max(hi[1], k.loc0 + k.nloc); } }
@@ -225,21 +247,27 @@ __device__ inline void plan_block(const PlanArgs &p, ROW row_keys) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       nvis[t] = __reduce_max_sync(0xffffffffu, nvis[t]); lo[t] = __reduce_min_sync(0xffffffffu, lo[t]); hi[t] = __reduce_max_sync(0xffffffffu, hi[t]);
+      if constexpr (WINDOWED) low[t] = __reduce_min_sync(0xffffffffu, low[t]);
     }
     if (lane < 3) {                                    // lane 0 / 1: the tiles, lane 2: the unit
       const int nv = lane == 0 ? nvis[0] : lane == 1 ? nvis[1] : max(nvis[0], nvis[1]);
       const int l = lane == 0 ? lo[0] : lane == 1 ? lo[1] : min(lo[0], lo[1]), h = lane == 0 ? hi[0] : lane == 1 ? hi[1] : max(hi[0], hi[1]);
       const bool two = row0 + p.spt < row_end;
-      const int n_cache = (nv + PAGE - 1) / PAGE, n_pages = n_cache + (h > l ? (h - l + PAGE - 1) / PAGE : 0);
+      int n_cache = (nv + PAGE - 1) / PAGE, skip = 0;
+      if constexpr (WINDOWED) {
+        skip = skipped_pages(lane == 0 ? low[0] : lane == 1 ? low[1] : min(low[0], low[1]), n_cache, p.sink_pages);
+        n_cache -= skip;
+      }
+      const int n_pages = n_cache + (h > l ? (h - l + PAGE - 1) / PAGE : 0);
       if (planned) {
-        keys[lane][u] = Keys{n_cache, n_pages, l};
+        keys[lane][u] = Keys{n_cache, n_pages, l, skip};
         const float us = n_pages * (lane == 2 && two ? PAIR_PAGE : SINGLE_PAGE);
         ent_us[lane == 2 ? u : p.n_units + 2 * u + lane] = us;
         atomicMax(&longest_us[lane == 2 ? 0 : 1], __float_as_int(us));
         if (lane == 0) { unit_row0[u] = row0; unit_rend[u] = row_end; unit_seq[u] = seq; }
       } else if (lane == 2) {                          // every unit one item, listed back to front (a causal pass lists its rows in ascending length)
         Item it{};
-        it.row0 = row0; it.row_end = row_end; it.seq = seq; it.p_end = n_pages; it.n_cache_pages = n_cache; it.loc_lo = l; it.pair = two;
+        it.row0 = row0; it.row_end = row_end; it.seq = seq; it.p_end = n_pages; it.n_cache_pages = n_cache; it.loc_lo = l; it.pair = two; it.skip = skip;
         p.items[p.n_units - 1 - u] = it;
       }
     }
@@ -320,7 +348,7 @@ __device__ inline void plan_block(const PlanArgs &p, ROW row_keys) {
     for (int j = lane; j < n; j += 32) {
       Item it{};
       it.row0 = unit_row0[u] + (paired ? 0 : (e & 1) * p.spt); it.row_end = unit_rend[u]; it.seq = unit_seq[u];
-      it.n_cache_pages = k.n_cache; it.loc_lo = k.loc_lo;
+      it.n_cache_pages = k.n_cache; it.loc_lo = k.loc_lo; it.skip = k.skip;
       it.p_begin = k.n_pages * j / n; it.p_end = k.n_pages * (j + 1) / n;      // (2^31 positions are 2^25 pages, in at most 2^5 pieces)
       it.pair = paired && unit_row0[u] + p.spt < unit_rend[u]; it.split = n > 1;
       p.items[place_s[e] + j] = it;
@@ -354,24 +382,50 @@ __device__ __forceinline__ Item direct_tile(const Args &a, int tile) {
   }
   return it;
 }
+// The same within a window, or over a caller's causal rows.
+__device__ __forceinline__ Item window_tile(const Args &a, int tile) {
+  const WindowRows &w = a.win.rows;
+  const int k = w.k, T = w.rows(), s = tile / a.direct.per_group, first = tile % a.direct.per_group * a.spt, last = min(first + a.spt, T) - 1;
+  const int n = min(w.seq_len[s], w.n_max);
+  Item it{};
+  it.row0 = s * T + first; it.row_end = (s + 1) * T; it.seq = s;
+  if (n < 0) return it;                                          // no pages: nothing is done, nothing written
+  int nvis = first < k ? n + min(last, k - 1) + 1 : 0, pos = first < k ? n + first : 0x7fffffff, local = 0;     // pos: no slot of the tile is at an earlier position
+  if (last >= k) {
+    const int b0 = (max(first, k) - k) / k, b1 = (last - k) / k;
+    nvis = max(nvis, n + b1 + 1); pos = min(pos, n + b0 + 1);
+    it.loc_lo = s * k * k + b0 * k;
+    local = ((b1 - b0 + 1) * k + PAGE - 1) / PAGE;
+  }
+  const int n_cache = (nvis + PAGE - 1) / PAGE;
+  it.skip = w.window > 0 ? skipped_pages(max(pos - w.window + 1, 0), n_cache, a.win.sink_pages) : 0;
+  it.n_cache_pages = n_cache - it.skip;
+  it.p_end = it.n_cache_pages + local;
+  return it;
+}
+template <int CACHE> __device__ __forceinline__ Item call_tile(const Args &a, int tile) { if constexpr (CACHE == PLAIN) return direct_tile(a, tile); else return window_tile(a, tile); }
 // Items that a tile of n_pages pages is cut into (three pages at least: see attention_direct), out of the places it has.
 __device__ __forceinline__ int direct_pieces(const Args &a, int n_pages) { return max(1, min(a.direct.pieces, n_pages / 3)); }
+template <int CACHE>
 __device__ __forceinline__ Item direct_item(const Args &a, int e) {
-  Item it = direct_tile(a, e / a.direct.pieces);
+  Item it = call_tile<CACHE>(a, e / a.direct.pieces);
   const int j = e % a.direct.pieces, n = direct_pieces(a, it.p_end), n_pages = it.p_end;
   it.split = n > 1;
   it.p_begin = j < n ? n_pages * j / n : 0; it.p_end = j < n ? n_pages * (j + 1) / n : 0;      // a place that is not used has no pages
   return it;
 }
 
+// 1 / l; rows of a caller's pages may see nothing at all (l = 0), and then are 0.
+template <int CACHE> __device__ __forceinline__ float over(float l) { return CACHE != PLAIN && !(l > 0.f) ? 0.f : 1.f / l; }
+
 // The end of a tile that its cluster does not share: both streams' halves merged and written.  A function of its own, called, so that its code does not
 // lie in the way of shared tiles (in place it cost them 0.1 - 0.2 us, as branches in their loop 0.3).
-template <int HD>
+template <int HD, int CACHE>
 __device__ __noinline__ void finish_alone(uint32_t o_addr, int t, int my_row, float m_ref, float l_run, int nj, bf16 *o, const float4 *xo, const float2 *xml) {
   const float2 other = xml[(1 - t) * 128 + my_row];
   const float M = fmaxf(m_ref, other.x);
   const float wm = m_ref == -INFINITY ? 0.f : exp2f(m_ref - M), wo = other.x == -INFINITY ? 0.f : exp2f(other.x - M);
-  const float inv = 1.f / (wm * l_run + wo * other.y);
+  const float inv = over<CACHE>(wm * l_run + wo * other.y);
 #pragma unroll 1
   for (int c = 0; c < HD / 2; c += 32) {
     uint32_t w[32];
@@ -414,8 +468,15 @@ __device__ __noinline__ void finish_alone(uint32_t o_addr, int t, int my_row, fl
 // (CLUSTER_MERGE).  Alone, 32/8 heads of 128, 272 rows, 1 k positions, clusters of two: 15.8 -> 13.2 us; 12/2 heads, four sequences of 72 rows, 1 k
 // positions, clusters of four: 16.5 -> 11.7.  1.5B-class step of 272 rows: 10.4 -> 8.1 us per layer; autoregressive step of 8 rows, where it replaces
 // a cut and the merge kernel: 5.1 + 3.4 -> 7.5 us.
-template <int HD, int STREAMS, bool DIRECT, bool AHEAD, bool CLUSTER>
-__global__ void __launch_bounds__(threads(STREAMS), 3 - STREAMS)
+// CACHE: calls over a caller's pages.  A tile's pages may lie apart (see Item::skip), rows see part of a page at either end of their window, a page of the
+// table may lie outside the pool, and what no row sees may hold anything.  Scores of what a row does not see are replaced, so K does no harm; a weight of
+// zero times a V that is not a number would, so such rows of V are zeroed: by the watcher, in the few pages that have any (WINDOW, and local rows), before it
+// releases their product.
+//   KV4: four more warps take the place of the page loads: each thread holds the codes of a row's half head, loaded two pages ahead straight from
+//   global memory, and stores them as bf16 in the layout a TMA load would have given them.  16 K elements of K and V per page cost 128 threads about
+//   250 instructions each; what a page of 1 us (pair) or 0.56 us (single) leaves idle.
+template <int HD, int STREAMS, bool DIRECT, bool AHEAD, bool CLUSTER, int CACHE>
+__global__ void __launch_bounds__(threads(STREAMS, CACHE), 3 - STREAMS)
 attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                const __grid_constant__ CUtensorMap tmKloc, const __grid_constant__ CUtensorMap tmVloc, const Args a, const TlSlot tl) {
   using L = Smem<HD, STREAMS, CLUSTER>;
@@ -434,8 +495,9 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
   if (threadIdx.x == 0) {
     ctl.abort_flag = 0;
     sm100::mbar_init(sm100::smem_u32(&ctl.q_full), 1);
-    for (int s = 0; s < L::K_STAGES; ++s) { sm100::mbar_init(sm100::smem_u32(&ctl.k_full[s]), 1); sm100::mbar_init(sm100::smem_u32(&ctl.k_empty[s]), 1); }
-    for (int s = 0; s < L::V_STAGES; ++s) { sm100::mbar_init(sm100::smem_u32(&ctl.v_full[s]), 1); sm100::mbar_init(sm100::smem_u32(&ctl.v_empty[s]), 1); }
+    constexpr int FILLERS = CACHE == KV4 ? 4 : 1;      // warps, or the one thread that issues a load
+    for (int s = 0; s < L::K_STAGES; ++s) { sm100::mbar_init(sm100::smem_u32(&ctl.k_full[s]), FILLERS); sm100::mbar_init(sm100::smem_u32(&ctl.k_empty[s]), 1); }
+    for (int s = 0; s < L::V_STAGES; ++s) { sm100::mbar_init(sm100::smem_u32(&ctl.v_full[s]), FILLERS); sm100::mbar_init(sm100::smem_u32(&ctl.v_empty[s]), 1); }
     for (int t = 0; t < STREAMS; ++t)
       for (int b = 0; b < 2; ++b) { sm100::mbar_init(sm100::smem_u32(&ctl.s_full[t][b]), 1); sm100::mbar_init(sm100::smem_u32(&ctl.p_full[t][b]), 4); }
     sm100::fence_mbar_init();
@@ -459,7 +521,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
   const int c_size = CLUSTER ? (int)sm100::cluster_size() : 1, c_rank = CLUSTER ? (int)sm100::cluster_rank() : 0;
   const int c_log = 31 - __clz(c_size);                // (a power of two: shifts instead of divisions ahead of the first loads, 0.1 us)
   const int kvh = (blockIdx.x >> c_log) % a.Hkv, item_no = (blockIdx.x >> c_log) / a.Hkv;
-  Item item = DIRECT ? direct_item(a, item_no) : a.items[item_no];   // all zero where the grid is larger than the plan: nothing to do
+  Item item = DIRECT ? direct_item<CACHE>(a, item_no) : a.items[item_no];   // all zero where the grid is larger than the plan: nothing to do
   const int np_item = item.p_end - item.p_begin;
   const bool sharing = CLUSTER && (!DIRECT || cluster_shares(np_item, c_log));     // (the same in all CTAs of a cluster)
   if constexpr (CLUSTER) {
@@ -471,6 +533,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
   const bool pair = STREAMS == 2 && !CLUSTER && item.pair != 0;
   const bool shared = STREAMS == 1 || pair;                            // every stream takes every page; otherwise two streams take them in turn
   const int ahead = shared ? 2 : 4;                                    // pages whose scores are computed ahead: two steps of every stream
+  // cached page number l of the item's sequence, in the table
+  auto table_at = [&](int l) { return CACHE != PLAIN && l >= a.win.sink_pages ? l + item.skip : l; };
   auto stream0 = [&](int p) { return shared ? 0 : p & 1; };            // streams [stream0(p), stream1(p)) take page p
   auto stream1 = [&](int p) { return pair ? 2 : stream0(p) + 1; };
   if (threadIdx.x == 0 && a.tile_count && np > 0) atomicAdd(a.tile_count, (unsigned long long)np * (pair ? 2 : 1));
@@ -490,7 +554,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       const uint64_t pol = sm100::policy_evict_last();
       const int32_t *table = a.page_table + (size_t)item.seq * a.pages_per_seq;
       const int n_table = min(item.n_cache_pages, item.p_end) - p_begin;         // pages of this item that the table backs
-      int cur = lane < n_table ? table[p_begin + lane] : 0, next = 0;
+      int cur = lane < n_table ? table[table_at(p_begin + lane)] : 0, next = 0;
       const CUtensorMap *tm = is_k ? &tmK : &tmV, *tm_loc = is_k ? &tmKloc : &tmVloc;
       const int base = is_k ? a.page_base_k : a.page_base_v;
       const int stages = is_k ? L::K_STAGES : L::V_STAGES;
@@ -511,10 +575,10 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
           }
           __syncwarp();
         }
-        if (p == np) break;
+        if (p == np || CACHE == KV4) break;              // (KV4: pages have warps of their own)
         if ((p & 31) == 0) {
           if (p) cur = next;
-          next = p + 32 + lane < n_table ? table[p_begin + p + 32 + lane] : 0;
+          next = p + 32 + lane < n_table ? table[table_at(p_begin + p + 32 + lane)] : 0;
         }
         const int page = __shfl_sync(0xffffffffu, cur, p & 31) + base;
         if (!sm100::mbar_wait_warp(empty0 + (uint32_t)s * 8u, ph, abortp)) break;
@@ -591,12 +655,40 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
     // are issued behind step j's.  After a failed wait that argument no longer holds, so from then on the watcher
     // meets the MMA warp at every barrier instead.
     bool failed = false;
-    auto release = [&](uint32_t id, uint32_t bar0, uint32_t par0, uint32_t bar1, uint32_t par1, uint32_t bar2, uint32_t par2) {
+    // Rows of a V page that no row of the call sees become zeros: positions behind the sequence's causal slots, those between the sinks and the window of its
+    // first slot, and local rows behind the sequence's own.
+    auto clear_unseen = [&](int p, uint32_t tile) {
+      const WindowRows &w = a.win.rows;
+      const int n = min(w.seq_len[item.seq], w.n_max), l = p_begin + p;
+      int from, gap0 = 0, gap1 = 0;                      // rows [gap0, gap1) and from `from` on
+      if (l < item.n_cache_pages) {
+        if constexpr (CACHE == KV4) return;              // (zeroed where the codes are read)
+        const int pos = table_at(l) * PAGE;
+        from = n + w.k - pos;
+        if (w.window > 0) { gap0 = w.sinks - pos; gap1 = n - w.window + 1 - pos; }
+      } else {
+        from = (item.seq + 1) * w.k * w.k - (item.loc_lo + (l - item.n_cache_pages) * PAGE);
+      }
+      if (from >= PAGE && (gap1 <= 0 || gap0 >= PAGE || gap0 >= gap1)) return;
+      for (int i = lane; i < PAGE * NH * 8; i += 32) {
+        const int row = i >> 3 & (PAGE - 1);
+        if (row >= from || (row >= gap0 && row < gap1)) sm100::st_shared_zero16(tile + (uint32_t)((i >> 9) * (PAGE * 128) + (i & 511) * 16));
+      }
+      sm100::fence_proxy_async();                        // (the product reads through the async proxy)
+      __syncwarp();
+    };
+    auto release = [&](uint32_t id, uint32_t bar0, uint32_t par0, uint32_t bar1, uint32_t par1, uint32_t bar2, uint32_t par2, int v_page = -1, uint32_t v_tile = 0) {
       if (!failed) {
         bool ok = true;
         if (lane == 0)
           ok = (!bar1 || sm100::mbar_wait(bar1, par1, abortp)) && (!bar2 || sm100::mbar_wait(bar2, par2, abortp)) && sm100::mbar_wait(bar0, par0, abortp);
         failed = !__shfl_sync(0xffffffffu, ok, 0);
+        if constexpr (CACHE != PLAIN) {
+          if (v_page >= 0 && !failed) {
+            failed = !sm100::mbar_wait_warp(bar1, par1, abortp);       // (complete: every lane sees the load)
+            clear_unseen(v_page, v_tile);
+          }
+        }
       }
       if (!failed) sm100::named_bar_arrive(id, 64);
       else sm100::named_bar_sync(id, 64);
@@ -609,22 +701,23 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       for (int t = stream0(p); t < stream1(p); ++t) {
         const bool first_stream = !pair || t == 0;
         release(1u + (uint32_t)(t * 2 + b), sm100::smem_u32(&ctl.p_full[t][b]), (uint32_t)(j >> 1) & 1u, first_stream ? sm100::smem_u32(&ctl.v_full[sv]) : 0u, phv,
-                first_stream && p + ahead < np ? sm100::smem_u32(&ctl.k_full[sk]) : 0u, phk);
+                first_stream && p + ahead < np ? sm100::smem_u32(&ctl.k_full[sk]) : 0u, phk, first_stream ? p : -1, smem0 + L::V_OFF + (uint32_t)sv * L::KV_BYTES);
       }
       if (++sv == L::V_STAGES) { sv = 0; phv ^= 1u; }
       if (++sk == L::K_STAGES) { sk = 0; phk ^= 1u; }
     }
-  } else if (warp >= 4) {
+  } else if (warp >= 4 && warp < 4 + 4 * STREAMS) {
     // ===================== softmax =====================
     const int tile = pair ? t : 0;
     const int nj = shared ? np : (np + 1 - t) >> 1;      // steps of this stream
     // (a row without a slot sees everything, so that its warp does not mask page after page for it)
-    int my_nvis = 0x7fffffff, my_loc0 = item.loc_lo, my_nloc = 1 << 30;
+    int my_nvis = 0x7fffffff, my_loc0 = item.loc_lo, my_nloc = 1 << 30, my_low = 0;
     {
       const int pr = row0 + tile * a.spt + my_row / a.G;
       if (my_row < rows_used && pr < item.row_end) {
         my_slot = pr;
-        if constexpr (DIRECT) { const RowKeys w = step_row_keys(a.direct.seq_len, a.direct.k, a.direct.n_max, pr); my_nvis = w.nvis; my_nloc = w.nloc; my_loc0 = w.loc0; }
+        if constexpr (CACHE != PLAIN) { const WindowKeys w = window_keys(a.win.rows, pr); my_nvis = w.nvis; my_nloc = w.nloc; my_loc0 = w.loc0; my_low = w.low; }
+        else if constexpr (DIRECT) { const RowKeys w = step_row_keys(a.direct.seq_len, a.direct.k, a.direct.n_max, pr); my_nvis = w.nvis; my_nloc = w.nloc; my_loc0 = w.loc0; }
         else { my_nvis = a.nvis[pr]; my_nloc = a.nloc[pr]; my_loc0 = a.loc0[pr]; }
       }
     }
@@ -636,6 +729,14 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
     auto wait_s = [&](int j) { return sm100::mbar_wait_warp(s_bar0 + (uint32_t)(j & 1) * 8u, (uint32_t)(j >> 1) & 1u, abortp); };
     float m_ref = -INFINITY, l_run = 0.f;
     bool ok = true;
+    // CACHE: which of 32 pages of this stream, from step j on, lie in the pool
+    auto pool_bits = [&](int j) {
+      const int l = p_begin + (shared ? j + lane : 2 * (j + lane) + t);
+      const int32_t *table = a.page_table + (size_t)item.seq * a.pages_per_seq;
+      return __ballot_sync(0xffffffffu, l < min(item.n_cache_pages, item.p_end) && (unsigned)__ldg(table + table_at(l)) < (unsigned)a.win.n_pages);
+    };
+    unsigned in_pool = 0;
+    if constexpr (CACHE != PLAIN) in_pool = pool_bits(0);
 #pragma unroll 1
     for (int j = AHEAD ? -1 : 0; j < nj; ++j) {          // (step -1: the walk)
       const bool live = !AHEAD || j >= 0;
@@ -652,11 +753,23 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       // for pages that are visible in full (all cached pages but the last ones of a row).
       {
         const int p = p_begin + (shared ? j : 2 * j + t);
-        int lo = 0, hi = 0;
+        int lo = 0, hi = 0, sink = 0;                    // (keys below `sink` too, in a windowed page)
+        if constexpr (CACHE != PLAIN) { if ((j & 31) == 0 && j > 0) in_pool = pool_bits(j); }
         if (!live) { }
-        else if (p < item.n_cache_pages) hi = my_nvis - p * PAGE;
+        else if (p < item.n_cache_pages) {
+          if constexpr (CACHE != PLAIN) {
+            const int pos = table_at(p) * PAGE;
+            if (in_pool >> (j & 31) & 1) { hi = my_nvis - pos; lo = my_low - pos; sink = min(a.win.rows.sinks - pos, hi); }
+          } else hi = my_nvis - p * PAGE;
+        }
         else if (my_nloc > 0) { lo = my_loc0 - (item.loc_lo + (p - item.n_cache_pages) * PAGE); hi = lo + my_nloc; }
-        if (lo > 0 || hi < PAGE) {
+        if (CACHE != PLAIN && sink > 0) {
+          if (hi < PAGE || (lo > 0 && sink < PAGE)) {
+#pragma unroll
+            for (int c = 0; c < PAGE; ++c)
+              if (c >= sink && (c < lo || c >= hi)) sv[c / 32][c & 31] = 0xff800000u;
+          }
+        } else if (lo > 0 || hi < PAGE) {
 #pragma unroll
           for (int c = 0; c < PAGE; ++c)
             if (c < lo || c >= hi) sv[c / 32][c & 31] = 0xff800000u;               // -inf
@@ -747,7 +860,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
     };
     if (shared) {
       if (ok && nj > 0) {
-        const float inv = item.split ? 1.f : 1.f / l_run;
+        const float inv = item.split ? 1.f : over<CACHE>(l_run);
 #pragma unroll
         for (int c = 0; c < HD; c += 32) { float v[32]; load32(c, v); write32(v, c, inv); }
         if (my_slot >= 0 && item.split) a.part_ml[part * 128 + my_row] = make_float2(m_ref, l_run);
@@ -777,7 +890,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         const float2 other = xml[(1 - t) * 128 + my_row];
         const float M = fmaxf(m_ref, other.x);
         const float wm = m_ref == -INFINITY ? 0.f : exp2f(m_ref - M), wo = other.x == -INFINITY ? 0.f : exp2f(other.x - M);
-        const float l = wm * l_run + wo * other.y, inv = CLUSTER || item.split ? 1.f : 1.f / l;
+        const float l = wm * l_run + wo * other.y, inv = CLUSTER || item.split ? 1.f : over<CACHE>(l);
 #pragma unroll
         for (int c = 0; c < HD / 2; c += 32) {
           float v[32];
@@ -812,25 +925,114 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         }
       }
       if constexpr (CLUSTER && DIRECT) {
-        if (ok && !sharing) finish_alone<HD>(o_addr, t, my_row, m_ref, l_run, nj, my_slot < 0 ? nullptr : o, xo, xml);
+        if (ok && !sharing) finish_alone<HD, CACHE>(o_addr, t, my_row, m_ref, l_run, nj, my_slot < 0 ? nullptr : o, xo, xml);
+      }
+    }
+  } else if (CACHE == KV4) {
+    // ===================== codes to tiles =====================
+    // A thread takes the same GP groups (of 32 dimensions) of one row of every page: lanes take rows, so codes are read 512 bytes at a time, and a quarter of
+    // a warp stores to eight different banks groups of the swizzled tile.  K runs `ahead` pages in front of V, as the products do: the watcher wants K of
+    // page p + ahead before it releases P V of page p.
+    constexpr int GP = HD / 64;
+    const int tid = threadIdx.x - threads(STREAMS), row = tid & 63, group0 = (tid >> 6) * GP;
+    struct Codes { uint4 c[GP]; uint32_t sb[GP]; };
+    if (np > 0) {
+      const WindowRows &w = a.win.rows;
+      const int n = min(w.seq_len[item.seq], w.n_max), n_table = min(item.n_cache_pages, item.p_end) - p_begin;
+      const int32_t *table = a.page_table + (size_t)item.seq * a.pages_per_seq;
+      // the table entry of page p is fetched two pages before the codes are, which are fetched two pages before they are stored
+      auto entry = [&](int p) { return p < n_table ? __ldg(table + table_at(p_begin + p)) : -1; };
+      auto codes = [&](const uint8_t *pool, int p, int page) {
+        Codes x;
+#pragma unroll
+        for (int e = 0; e < GP; ++e) { x.c[e] = make_uint4(0, 0, 0, 0); x.sb[e] = 0; }
+        if (p < n_table && (unsigned)page < (unsigned)a.win.n_pages) {
+          const uint8_t *rec = pool + ((size_t)page * a.Hkv + kvh) * kv4::record_bytes(HD);
+          const int pos = table_at(p_begin + p) * PAGE + row;
+#pragma unroll
+          for (int e = 0; e < GP; ++e) x.c[e] = __ldg(reinterpret_cast<const uint4 *>(rec + ((group0 + e) * PAGE + row) * 16));
+          if (pos < n + w.k && (w.window == 0 || pos < w.sinks || pos > n - w.window)) {      // what no row sees stands for zeros: scale and base 0
+#pragma unroll
+            for (int e = 0; e < GP; ++e) x.sb[e] = __ldg(reinterpret_cast<const uint32_t *>(rec + kv4::code_bytes(HD) + (row * (HD / 32) + group0 + e) * 4));
+          }
+        }
+        return x;
+      };
+      auto store = [&](const Codes &x, uint32_t tile) {
+#pragma unroll
+        for (int e = 0; e < GP; ++e) {
+          const uint32_t ss = kv4::low_twice(x.sb[e]), bb = kv4::high_twice(x.sb[e]);
+          const uint32_t wd[4] = {x.c[e].x, x.c[e].y, x.c[e].z, x.c[e].w};
+          const uint32_t line = tile + (uint32_t)(((group0 + e) >> 1) * (PAGE * 128) + row * 128);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t v[4];
+            kv4::values8(wd[i], ss, bb, v);
+            sm100::st_shared_v4(line + (uint32_t)(((((group0 + e) & 1) * 4 + i) ^ (row & 7)) << 4), v[0], v[1], v[2], v[3]);
+          }
+        }
+        sm100::fence_proxy_async();
+        __syncwarp();
+      };
+      // one page of K or V into its stage; local rows come by TMA
+      auto fill = [&](const Codes &x, int p, bool is_k) {
+        const int stages = is_k ? L::K_STAGES : L::V_STAGES, s = p % stages;
+        const uint32_t full = sm100::smem_u32(is_k ? &ctl.k_full[s] : &ctl.v_full[s]), empty = sm100::smem_u32(is_k ? &ctl.k_empty[s] : &ctl.v_empty[s]);
+        const uint32_t tile = smem0 + (is_k ? L::K_OFF : L::V_OFF) + (uint32_t)s * L::KV_BYTES;
+        if (!sm100::mbar_wait_warp(empty, (uint32_t)(p / stages + 1) & 1u, abortp)) return false;
+        if (p < n_table) {
+          store(x, tile);
+          if (lane == 0) sm100::mbar_arrive(full);
+        } else if (tid < 32) {
+          if (sm100::elect_one()) {
+            sm100::mbar_expect_tx(full, (uint32_t)L::KV_BYTES);
+            sm100::tma_load_4d(tile, is_k ? &tmKloc : &tmVloc, full, 0, item.loc_lo + (p_begin + p - item.n_cache_pages) * PAGE, 0, kvh, sm100::policy_evict_last());
+          }
+          __syncwarp();
+        } else if (lane == 0) {
+          sm100::mbar_arrive(full);
+        }
+        __syncwarp();
+        return true;
+      };
+      pdl_wait();
+      int ke[2] = {entry(2), entry(3)}, ve[2] = {ke[0], ke[1]};
+      const int e0 = entry(0), e1 = entry(1);
+      Codes k0 = codes(a.win.k4, 0, e0), k1 = codes(a.win.k4, 1, e1), v0 = codes(a.win.v4, 0, e0), v1 = codes(a.win.v4, 1, e1);
+      bool ok = true;
+      auto next_k = [&](int p) {
+        ok = fill(k0, p, true);
+        k0 = k1; k1 = codes(a.win.k4, p + 2, ke[0]);
+        ke[0] = ke[1]; ke[1] = entry(p + 4);
+      };
+      auto next_v = [&](int p) {
+        ok = fill(v0, p, false);
+        v0 = v1; v1 = codes(a.win.v4, p + 2, ve[0]);
+        ve[0] = ve[1]; ve[1] = entry(p + 4);
+      };
+      for (int p = 0; ok && p < min(ahead, np); ++p) next_k(p);
+      for (int p = 0; ok && p < np; ++p) {
+        next_v(p);
+        if (ok && p + ahead < np) next_k(p + ahead);
       }
     }
   }
   if constexpr (CLUSTER) {
-    if (warp < 4) sm100::cluster_wait();
+    if (warp < 4 || warp >= 4 + 4 * STREAMS) sm100::cluster_wait();
     if (sharing) sm100::cluster_sync();                  // the stores to one another have arrived
-    if (sharing && warp >= 4 && np_item > 0 && my_slot >= 0) {
+    if (sharing && warp >= 4 && warp < 4 + 4 * STREAMS && np_item > 0 && my_slot >= 0) {
       const float2 *ml = reinterpret_cast<const float2 *>(smem_raw + L::PEER_ML_OFF) + my_row;
       const float4 *x = reinterpret_cast<const float4 *>(smem_raw + L::PEER_OFF) + t * (c_cols / 4) * 128 + my_row;
       float M = -INFINITY, den = 0.f;
       for (int r = 0; r < c_size; ++r) M = fmaxf(M, ml[r * 128].x);
-      for (int r = 0; r < c_size; ++r) den += exp2f(ml[r * 128].x - M) * ml[r * 128].y;
-      const float inv = 1.f / den;
+      auto weight = [&](float m) { return CACHE != PLAIN && m == -INFINITY ? 0.f : exp2f(m - M); };
+      for (int r = 0; r < c_size; ++r) den += weight(ml[r * 128].x) * ml[r * 128].y;
+      const float inv = over<CACHE>(den);
       bf16 *o = a.O + ((size_t)my_slot * a.Hq + kvh * a.G + my_row % a.G) * HD + t * (HD / 2) + c_rank * c_cols;
       for (int g = 0; g < c_cols / 4; g += 2) {          // eight columns
         float acc[8] = {};
         for (int r = 0; r < c_size; ++r) {
-          const float w = exp2f(ml[r * 128].x - M);      // (a CTA without pages: 0)
+          const float w = weight(ml[r * 128].x);         // (a CTA without pages: 0)
           const float4 u = x[(r * 2 * (c_cols / 4) + g) * 128], v = x[(r * 2 * (c_cols / 4) + g + 1) * 128];
           acc[0] = fmaf(w, u.x, acc[0]); acc[1] = fmaf(w, u.y, acc[1]); acc[2] = fmaf(w, u.z, acc[2]); acc[3] = fmaf(w, u.w, acc[3]);
           acc[4] = fmaf(w, v.x, acc[4]); acc[5] = fmaf(w, v.y, acc[5]); acc[6] = fmaf(w, v.z, acc[6]); acc[7] = fmaf(w, v.w, acc[7]);
@@ -864,7 +1066,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
 // Merge the partial results of the query tiles that were split: O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.
 // HD / 16 blocks of 256 threads per (query tile, KV head); a thread takes 8 columns of one MMA row, neighbouring
 // threads neighbouring rows, which is how the partial results lie in memory.
-template <int HD, bool DIRECT>
+template <int HD, bool DIRECT, int CACHE>
 __global__ void __launch_bounds__(256)
 attn_combine_kernel(const Args a, TlSlot tl) {
   pdl_trigger();
@@ -874,7 +1076,7 @@ attn_combine_kernel(const Args a, TlSlot tl) {
   const int cg = (blockIdx.x % BLOCKS) * 2 + (threadIdx.x >> 7), m = threadIdx.x & 127;
   Tile t{};
   if constexpr (DIRECT) {
-    const Item it = direct_tile(a, w / a.Hkv);
+    const Item it = call_tile<CACHE>(a, w / a.Hkv);
     t.row0 = it.row0; t.row_end = it.row_end; t.n_items = direct_pieces(a, it.p_end); t.item0 = w / a.Hkv * a.direct.pieces;
   } else {
     t = a.tiles[w / a.Hkv];
@@ -912,7 +1114,7 @@ attn_combine_kernel(const Args a, TlSlot tl) {
         acc[4] = fmaf(wgt, y[u].x, acc[4]); acc[5] = fmaf(wgt, y[u].y, acc[5]); acc[6] = fmaf(wgt, y[u].z, acc[6]); acc[7] = fmaf(wgt, y[u].w, acc[7]);
       }
     }
-    const float inv = 1.f / den;
+    const float inv = over<CACHE>(den);
     __nv_bfloat162 h0 = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv), h1 = __floats2bfloat162_rn(acc[2] * inv, acc[3] * inv),
                    h2 = __floats2bfloat162_rn(acc[4] * inv, acc[5] * inv), h3 = __floats2bfloat162_rn(acc[6] * inv, acc[7] * inv);
     uint4 u;

@@ -183,6 +183,13 @@ __global__ void __launch_bounds__(512) attn_meta_plan_kernel(RowMeta m, const in
   m.seq[r] = w.seq; m.nvis[r] = w.nvis; m.loc0[r] = w.loc0; m.nloc[r] = w.nloc;
 }
 
+// The plan alone, of a call over a caller's pages (whose rows' keys follow from the lengths).
+__global__ void __launch_bounds__(512) attn_window_plan_kernel(WindowRows w, attn_tc::PlanArgs plan) {
+  pdl_trigger();
+  pdl_wait();
+  attn_tc::plan_block(plan, [&](int r) { return window_keys(w, r); });
+}
+
 // What every layer of a pass shares, computed once per pass from the row metadata: cos/sin of
 // pos * theta^(-2i/hd) (evaluated in double, stored as float), one thread per (row, i), and, when
 // plan.tiles is set, the attention work plan (the first block).

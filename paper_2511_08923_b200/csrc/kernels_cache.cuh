@@ -1,5 +1,5 @@
 // A paged cache that the caller keeps: page map of a batch, K and V rows held in 4 bits, and the plain attention over such pages or bf16
-// pages with a sliding window.  (The kernel for few rows over 4-bit pages: attn_few.cuh.)
+// pages with a sliding window.  (The tensor-core kernels over them: attn_few.cuh, attn_tc.cuh.)
 #pragma once
 #include "common.cuh"
 

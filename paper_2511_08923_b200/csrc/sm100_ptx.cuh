@@ -160,6 +160,12 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
+// Plain stores to shared memory by its address.
+__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void st_shared_zero16(uint32_t addr) { st_shared_v4(addr, 0u, 0u, 0u, 0u); }
+
 // ---- CTA pairs (clusters of two) -----------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;

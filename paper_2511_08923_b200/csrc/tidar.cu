@@ -479,11 +479,11 @@ int gemm_partials(tidar_ctx *c, const bf16 *A, int a_rows, const bf16 *W, const 
 }
 
 // bf16 tensor maps for the attention kernel (128-byte swizzle, 64-element inner box).
-bool encode_q_map(tidar_ctx *c, CUtensorMap *tm, const void *q, int rows) {
+bool encode_q_map(tidar_ctx *c, CUtensorMap *tm, const void *q, int rows, long long row_stride = 0) {
   const tidar_config &cf = c->cfg;
   const int G = cf.n_q_heads / cf.n_kv_heads, spt = 128 / G;
   cuuint64_t dims[3] = {(cuuint64_t)cf.head_dim, (cuuint64_t)cf.n_q_heads, (cuuint64_t)rows};
-  cuuint64_t strides[2] = {(cuuint64_t)cf.head_dim * 2, (cuuint64_t)cf.n_q_heads * cf.head_dim * 2};
+  cuuint64_t strides[2] = {(cuuint64_t)cf.head_dim * 2, row_stride ? (cuuint64_t)row_stride * 2 : (cuuint64_t)cf.n_q_heads * cf.head_dim * 2};
   cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)spt}, es[3] = {1, 1, 1};
   return c->encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(q), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -499,11 +499,11 @@ bool encode_pages_map(tidar_ctx *c, CUtensorMap *tm, const void *pool, long long
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // Step-local K or V rows [row][kv head][head_dim]; a load brings 64 rows in the layout of a page.
-bool encode_local_map(tidar_ctx *c, CUtensorMap *tm, const void *loc, long long rows) {
+bool encode_local_map(tidar_ctx *c, CUtensorMap *tm, const void *loc, long long rows, long long row_stride = 0) {
   const tidar_config &cf = c->cfg;
   const cuuint64_t head = (cuuint64_t)cf.head_dim * 2;
   cuuint64_t dims[4] = {64, (cuuint64_t)rows, (cuuint64_t)cf.head_dim / 64, (cuuint64_t)cf.n_kv_heads};
-  cuuint64_t strides[3] = {(cuuint64_t)cf.n_kv_heads * head, 128, head};
+  cuuint64_t strides[3] = {row_stride ? (cuuint64_t)row_stride * 2 : (cuuint64_t)cf.n_kv_heads * head, 128, head};
   cuuint32_t box[4] = {64, 64, (cuuint32_t)cf.head_dim / 64, 1}, es[4] = {1, 1, 1, 1};
   return c->encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(loc), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -641,33 +641,33 @@ attn_tc::Args attention_args(const tidar_ctx *c, const AttnMaps &m, const KvGeom
   return a;
 }
 // One CTA per item, or (cluster > 1) a cluster of CTAs per item.
-template <int STREAMS, bool DIRECT, bool AHEAD = false>
+template <int STREAMS, bool DIRECT, bool AHEAD = false, int CACHE = attn_tc::PLAIN>
 void launch_attention_kernel(tidar_ctx *c, int grid, const AttnMaps &m, const attn_tc::Args &a, int cluster = 1) {
   Launch l(c, TIDAR_TC_ATTN);
-  const int threads = attn_tc::threads(STREAMS);
-  if constexpr (STREAMS == 2) {
+  const int threads = attn_tc::threads(STREAMS, CACHE);
+  if constexpr (STREAMS == 2 && (DIRECT || CACHE == attn_tc::PLAIN)) {      // (calls over a caller's pages share items only where they have no plan)
     if (cluster > 1) {
       if (c->cfg.head_dim == 128)
-        launch_pdl_cluster(cluster, attn_tc::attn_tc_kernel<128, 2, DIRECT, AHEAD, true>, grid * cluster, threads, attn_tc::Smem<128, 2, true>::TOTAL, c->stream, *m.q, *m.k,
+        launch_pdl_cluster(cluster, attn_tc::attn_tc_kernel<128, 2, DIRECT, AHEAD, true, CACHE>, grid * cluster, threads, attn_tc::Smem<128, 2, true>::TOTAL, c->stream, *m.q, *m.k,
                            *m.v, *m.kloc, *m.vloc, a, l.tl);
       else
-        launch_pdl_cluster(cluster, attn_tc::attn_tc_kernel<64, 2, DIRECT, AHEAD, true>, grid * cluster, threads, attn_tc::Smem<64, 2, true>::TOTAL, c->stream, *m.q, *m.k,
+        launch_pdl_cluster(cluster, attn_tc::attn_tc_kernel<64, 2, DIRECT, AHEAD, true, CACHE>, grid * cluster, threads, attn_tc::Smem<64, 2, true>::TOTAL, c->stream, *m.q, *m.k,
                            *m.v, *m.kloc, *m.vloc, a, l.tl);
       return;
     }
   }
   if (c->cfg.head_dim == 128)
-    launch_pdl(attn_tc::attn_tc_kernel<128, STREAMS, DIRECT, AHEAD, false>, grid, threads, attn_tc::Smem<128, STREAMS>::TOTAL, c->stream, *m.q, *m.k, *m.v, *m.kloc, *m.vloc, a, l.tl);
+    launch_pdl(attn_tc::attn_tc_kernel<128, STREAMS, DIRECT, AHEAD, false, CACHE>, grid, threads, attn_tc::Smem<128, STREAMS>::TOTAL, c->stream, *m.q, *m.k, *m.v, *m.kloc, *m.vloc, a, l.tl);
   else
-    launch_pdl(attn_tc::attn_tc_kernel<64, STREAMS, DIRECT, AHEAD, false>, grid, threads, attn_tc::Smem<64, STREAMS>::TOTAL, c->stream, *m.q, *m.k, *m.v, *m.kloc, *m.vloc, a, l.tl);
+    launch_pdl(attn_tc::attn_tc_kernel<64, STREAMS, DIRECT, AHEAD, false, CACHE>, grid, threads, attn_tc::Smem<64, STREAMS>::TOTAL, c->stream, *m.q, *m.k, *m.v, *m.kloc, *m.vloc, a, l.tl);
 }
 
-template <bool DIRECT>
+template <bool DIRECT, int CACHE = attn_tc::PLAIN>
 void launch_attention_merge(tidar_ctx *c, int tiles, const attn_tc::Args &a) {
   Launch l(c, TIDAR_TC_ATTN);
   const int blocks = tiles * (c->cfg.head_dim / 16);
-  if (c->cfg.head_dim == 128) launch_pdl(attn_tc::attn_combine_kernel<128, DIRECT>, blocks, 256, 0, c->stream, a, l.tl);
-  else launch_pdl(attn_tc::attn_combine_kernel<64, DIRECT>, blocks, 256, 0, c->stream, a, l.tl);
+  if (c->cfg.head_dim == 128) launch_pdl(attn_tc::attn_combine_kernel<128, DIRECT, CACHE>, blocks, 256, 0, c->stream, a, l.tl);
+  else launch_pdl(attn_tc::attn_combine_kernel<64, DIRECT, CACHE>, blocks, 256, 0, c->stream, a, l.tl);
 }
 
 bool merges(const attn_tc::PlanArgs &p) { return p.max_items > p.n_units && p.max_pieces > 1; }
@@ -684,7 +684,7 @@ void launch_attention_tc(tidar_ctx *c, const attn_tc::PlanArgs &p, const AttnMap
 }
 
 // How a stand-alone call goes without a plan, every CTA working out its own item: streams per CTA (0 = planned) and items per query tile.
-// n_pages: pages a sequence may have (its length is on the device).  The plan kernel costs 4.5 us, which a pass pays once for all
+// rows: of a sequence; n_pages: pages a sequence may have (its length is on the device).  The plan kernel costs 4.5 us, which a pass pays once for all
 // layers but such a call alone; cutting a key range into p items saves (1 - 1/p) of 0.56 us per page and costs about 6 + 0.3 p us
 // (partial results, merge kernel).
 //   Where every tile may have as many SMs as it can use, sqrt(0.56 n_pages / 0.3), there is nothing to distribute: uncut up to 15 pages, cut
@@ -696,9 +696,9 @@ void launch_attention_tc(tidar_ctx *c, const attn_tc::PlanArgs &p, const AttnMap
 //     two.  Four sequences of 1 k positions there (288 tiles): 42.1 us planned, 25.7 this way, at 9 k 175 and 148; but a plan evens
 //     out ragged lengths, which pays from about 60 pages on (lengths between 2 k and 4 k: 53.9 planned, 58.1 not).
 struct DirectPlan { int streams, pieces, cluster; };
-DirectPlan attention_direct(const tidar_ctx *c, int n_seqs, int k, int n_pages) {
+DirectPlan attention_direct(const tidar_ctx *c, int n_seqs, int rows, int n_pages) {
   const int spt = 128 / (c->cfg.n_q_heads / c->cfg.n_kv_heads);
-  const long long tiles = (long long)n_seqs * ((k * (k + 1) + spt - 1) / spt) * c->cfg.n_kv_heads;
+  const long long tiles = (long long)n_seqs * ((rows + spt - 1) / spt) * c->cfg.n_kv_heads;
   if (tiles > c->n_sms) return {tiles <= 2 * c->n_sms && n_pages <= 40 ? 1 : 0, 1, 1};
   const int most = std::min<int>(attn_tc::MAX_SPLITS, c->n_sms / (int)tiles);
   const int pieces = (int)sqrt(1.9 * n_pages);
@@ -727,6 +727,55 @@ void launch_attention(tidar_ctx *c, const bf16 *Q, const bf16 *Kp, const bf16 *V
 
 // 4-bit pages: sequences of so few rows per KV head go through attn_few_kernel.
 bool few_rows(const tidar_ctx *c, const WindowRows &w) { return w.rows() * (c->cfg.n_q_heads / c->cfg.n_kv_heads) <= 2 * attn_few::ROWS; }
+
+// Calls over a caller's pages on the tensor cores: as tidar_attention's (see attention_direct), except that a tile's pages are those of its window, and that
+// 4-bit pages have no instance of one stream (its warps and the four that turn codes into tiles would not fit an SM twice).
+template <int CACHE>
+int launch_cache_attention(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
+  const WindowRows &w = x.rows;
+  const int T = w.rows(), R = n_seqs * T, spt = 128 / (x.Hq / x.Hkv);
+  // pages that a tile may need: its window's, which begins and ends inside a page, and the sinks'
+  const int span = w.blocks ? 2 * w.k : std::min(spt, T);
+  const int sink_pages = w.window > 0 ? (int)std::min<long long>(((long long)w.sinks + 63) / 64, x.width) : 0;
+  const int n_pages = w.window > 0 ? (int)std::min<long long>(x.width, ((long long)w.window + span) / 64 + 2 + sink_pages) : x.width;
+  DirectPlan d = attention_direct(c, n_seqs, T, n_pages);
+  if (CACHE == attn_tc::KV4 && d.streams == 1) d.streams = 0;
+  attn_tc::PlanArgs plan{};
+  if (!d.streams) {
+    c->split_keys = may_split((int)std::min<long long>((long long)n_pages * 64, INT32_MAX)); c->attn_cluster = 1;
+    plan = attention_plan(c, R, T);
+    plan.sink_pages = sink_pages;
+    note_route(c, plan);
+    Launch l(c, TIDAR_TC_EMBED);
+    launch_pdl(attn_window_plan_kernel, 1, 512, 0, c->stream, w, plan);
+  }
+  CUtensorMap tq, tk, tv, tkl, tvl;
+  bool ok = encode_q_map(c, &tq, x.q, R, x.q_stride);
+  tk = tv = tkl = tvl = tq;                              // (those that no load uses)
+  if (CACHE == attn_tc::WINDOW) ok = ok && encode_pages_map(c, &tk, x.k_pages, x.n_pages) && encode_pages_map(c, &tv, x.v_pages, x.n_pages);
+  if (w.blocks) ok = ok && encode_local_map(c, &tkl, x.k_local, (long long)n_seqs * w.k * w.k, x.local_stride) && encode_local_map(c, &tvl, x.v_local, (long long)n_seqs * w.k * w.k, x.local_stride);
+  if (!ok) return fail(c, TIDAR_ECUDA, "cuTensorMapEncodeTiled failed for an attention operand");
+  const AttnMaps am{&tq, &tk, &tv, &tkl, &tvl, 0, 0};
+  KvGeom g{};
+  g.page_table = x.table; g.pages_per_seq = x.width;
+  attn_tc::Args a = attention_args(c, am, g, x.out);
+  a.win = attn_tc::Window{w, sink_pages, x.n_pages, (const uint8_t *)x.k_pages, (const uint8_t *)x.v_pages};
+  if (d.streams) {
+    c->route = {d.cluster, d.pieces > 1, 0};
+    a.direct.pieces = d.pieces; a.direct.per_group = (T + spt - 1) / spt;
+    const int tiles = n_seqs * a.direct.per_group * a.Hkv;
+    if constexpr (CACHE == attn_tc::WINDOW) {
+      if (d.streams == 1) { launch_attention_kernel<1, true, false, CACHE>(c, tiles, am, a); return TIDAR_OK; }
+    }
+    launch_attention_kernel<2, true, false, CACHE>(c, tiles * d.pieces, am, a, d.cluster);
+    if (d.pieces > 1) launch_attention_merge<true, CACHE>(c, tiles, a);
+  } else {
+    a.items = plan.items; a.tiles = plan.tiles;
+    launch_attention_kernel<2, false, false, CACHE>(c, plan.max_items * plan.Hkv, am, a);
+    if (merges(plan)) launch_attention_merge<false, CACHE>(c, 2 * plan.n_units * plan.Hkv, a);
+  }
+  return TIDAR_OK;
+}
 
 void launch_few(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
   Launch l(c, TIDAR_TC_ATTN);
@@ -887,6 +936,23 @@ int forward_rows(tidar_ctx *c, int R, bool with_head, int rows_per_group, const 
   return TIDAR_OK;
 }
 
+// Shared memory that the attention kernels over a caller's pages may claim.
+template <int HD, int CACHE>
+cudaError_t cache_attention_smem() {
+  using namespace attn_tc;
+  auto smem = [](const void *f, int bytes) { return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
+  cudaError_t e = smem((const void *)attn_tc_kernel<HD, 2, false, false, false, CACHE>, Smem<HD, 2>::TOTAL);
+  if (e == cudaSuccess) e = smem((const void *)attn_tc_kernel<HD, 2, true, false, false, CACHE>, Smem<HD, 2>::TOTAL);
+  if (e == cudaSuccess) e = smem((const void *)attn_tc_kernel<HD, 2, true, false, true, CACHE>, Smem<HD, 2, true>::TOTAL);
+  if constexpr (CACHE == WINDOW) {
+    const void *f = (const void *)attn_tc_kernel<HD, 1, true, false, false, CACHE>;
+    if (e == cudaSuccess) e = smem(f, Smem<HD, 1>::TOTAL);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  }
+  return e;
+}
+template <int CACHE> cudaError_t cache_attention_attributes(int head_dim) { return head_dim == 128 ? cache_attention_smem<128, CACHE>() : cache_attention_smem<64, CACHE>(); }
+
 // Driver entry point for tensor-map encoding (resolved through the runtime so that the
 // library has no link-time dependency on the driver), tensor maps of every weight
 // matrix, kernel attributes.
@@ -926,20 +992,20 @@ int init_tensor_core_path(tidar_ctx *c) {
     auto smem = [](const void *f, int bytes) { return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
     CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<128>, attn_few::Smem<128>::TOTAL));
     CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<64>, attn_few::Smem<64>::TOTAL));
-    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 2, false, false, false>, attn_tc::Smem<128, 2>::TOTAL));
-    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 2, false, true, false>, attn_tc::Smem<128, 2>::TOTAL));
-    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<64, 2, false, false, false>, attn_tc::Smem<64, 2>::TOTAL));
-    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<64, 2, false, true, false>, attn_tc::Smem<64, 2>::TOTAL));
-    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 2, true, false, false>, attn_tc::Smem<128, 2>::TOTAL));
-    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<64, 2, true, false, false>, attn_tc::Smem<64, 2>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 2, false, false, false, 0>, attn_tc::Smem<128, 2>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 2, false, true, false, 0>, attn_tc::Smem<128, 2>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<64, 2, false, false, false, 0>, attn_tc::Smem<64, 2>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<64, 2, false, true, false, 0>, attn_tc::Smem<64, 2>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 2, true, false, false, 0>, attn_tc::Smem<128, 2>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<64, 2, true, false, false, 0>, attn_tc::Smem<64, 2>::TOTAL));
     auto clusters = [&](auto kernel_128, auto kernel_64) {
       const void *f = cf.head_dim == 128 ? (const void *)kernel_128 : (const void *)kernel_64;
       const int bytes = cf.head_dim == 128 ? attn_tc::Smem<128, 2, true>::TOTAL : attn_tc::Smem<64, 2, true>::TOTAL;
       return smem(f, bytes);
     };
-    CUDA_TRY(c, clusters(attn_tc::attn_tc_kernel<128, 2, false, false, true>, attn_tc::attn_tc_kernel<64, 2, false, false, true>));
-    CUDA_TRY(c, clusters(attn_tc::attn_tc_kernel<128, 2, false, true, true>, attn_tc::attn_tc_kernel<64, 2, false, true, true>));
-    CUDA_TRY(c, clusters(attn_tc::attn_tc_kernel<128, 2, true, false, true>, attn_tc::attn_tc_kernel<64, 2, true, false, true>));
+    CUDA_TRY(c, clusters(attn_tc::attn_tc_kernel<128, 2, false, false, true, 0>, attn_tc::attn_tc_kernel<64, 2, false, false, true, 0>));
+    CUDA_TRY(c, clusters(attn_tc::attn_tc_kernel<128, 2, false, true, true, 0>, attn_tc::attn_tc_kernel<64, 2, false, true, true, 0>));
+    CUDA_TRY(c, clusters(attn_tc::attn_tc_kernel<128, 2, true, false, true, 0>, attn_tc::attn_tc_kernel<64, 2, true, false, true, 0>));
     for (int size = 2; size <= attn_tc::MAX_CLUSTER && size * 16 <= cf.head_dim; size *= 2) {
       cudaLaunchConfig_t lc{};
       lc.gridDim = dim3(size); lc.blockDim = dim3(attn_tc::threads(2));
@@ -948,11 +1014,13 @@ int init_tensor_core_path(tidar_ctx *c) {
       at[0].id = cudaLaunchAttributeClusterDimension;
       at[0].val.clusterDim.x = size; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
       lc.attrs = at; lc.numAttrs = 1;
-      CUDA_TRY(c, cudaOccupancyMaxActiveClusters(&c->max_clusters[size], cf.head_dim == 128 ? (const void *)attn_tc::attn_tc_kernel<128, 2, false, false, true>
-                                                                                            : (const void *)attn_tc::attn_tc_kernel<64, 2, false, false, true>, &lc));
+      CUDA_TRY(c, cudaOccupancyMaxActiveClusters(&c->max_clusters[size], cf.head_dim == 128 ? (const void *)attn_tc::attn_tc_kernel<128, 2, false, false, true, 0>
+                                                                                            : (const void *)attn_tc::attn_tc_kernel<64, 2, false, false, true, 0>, &lc));
     }
-    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 1, true, false, false>, attn_tc::Smem<128, 1>::TOTAL));
-    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<64, 1, true, false, false>, attn_tc::Smem<64, 1>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 1, true, false, false, 0>, attn_tc::Smem<128, 1>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<64, 1, true, false, false, 0>, attn_tc::Smem<64, 1>::TOTAL));
+    CUDA_TRY(c, cache_attention_attributes<attn_tc::WINDOW>(cf.head_dim));
+    CUDA_TRY(c, cache_attention_attributes<attn_tc::KV4>(cf.head_dim));
   }
   {
     auto max_smem_split = [&](const void *f) { return cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared); };
@@ -960,8 +1028,8 @@ int init_tensor_core_path(tidar_ctx *c) {
                              (const void *)rope_kv_kernel<1, false, float>, (const void *)rope_kv_kernel<MAX_SLABS, false, float>, (const void *)rope_kv_kernel<MAX_SLABS, false, bf16>,
                              (const void *)rope_kv_kernel<1, true, float>, (const void *)rope_kv_kernel<MAX_SLABS, true, float>,
                              (const void *)swiglu_slab_kernel<float>, (const void *)swiglu_slab_kernel<bf16>,
-                             (const void *)attn_tc::attn_combine_kernel<128, false>, (const void *)attn_tc::attn_combine_kernel<64, false>,
-                             (const void *)attn_tc::attn_combine_kernel<128, true>, (const void *)attn_tc::attn_combine_kernel<64, true>,
+                             (const void *)attn_tc::attn_combine_kernel<128, false, 0>, (const void *)attn_tc::attn_combine_kernel<64, false, 0>,
+                             (const void *)attn_tc::attn_combine_kernel<128, true, 0>, (const void *)attn_tc::attn_combine_kernel<64, true, 0>,
                              (const void *)mix_rows_kernel, (const void *)argmax_merge_kernel, (const void *)verify_select_kernel, (const void *)stage_step_kernel};
     for (const void *f : kernels) CUDA_TRY(c, max_smem_split(f));
     std::vector<const void *> norms = {(const void *)rmsnorm_bulk_kernel<512, 1>, (const void *)rmsnorm_bulk_kernel<512, 2>, (const void *)rmsnorm_bulk_kernel<512, 3>,
@@ -980,8 +1048,8 @@ int init_tensor_core_path(tidar_ctx *c) {
       CUDA_TRY(c, max_smem_split(f));
       CUDA_TRY(c, cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_SMEM));
     }
-    CUDA_TRY(c, max_smem_split((const void *)attn_tc::attn_tc_kernel<128, 1, true, false, false>));
-    CUDA_TRY(c, max_smem_split((const void *)attn_tc::attn_tc_kernel<64, 1, true, false, false>));
+    CUDA_TRY(c, max_smem_split((const void *)attn_tc::attn_tc_kernel<128, 1, true, false, false, 0>));
+    CUDA_TRY(c, max_smem_split((const void *)attn_tc::attn_tc_kernel<64, 1, true, false, false, 0>));
   }
   const int max_smem = gemm_tc::SMEM_BUDGET + 1024;
   CUDA_TRY(c, cudaFuncSetAttribute(gemm_tc::gemm_tc_kernel<gemm_tc::MODE_SLAB, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, max_smem));
@@ -1904,7 +1972,7 @@ int tidar_attention(tidar_ctx *c, const void *q, const void *k_pages, const void
   const int R = n_seqs * k * (k + 1), n_max = pages_per_seq * c->cfg.page_size - k;
   const KvGeom g{c->cfg.n_kv_heads, c->cfg.head_dim, c->cfg.page_size, pages_per_seq, page_table, n_pages};
   if (c->cfg.impl == 0) {
-    const DirectPlan d = attention_direct(c, n_seqs, k, pages_per_seq);
+    const DirectPlan d = attention_direct(c, n_seqs, k * (k + 1), pages_per_seq);
     attn_tc::PlanArgs plan{};
     if (!d.streams) {                              // (launched ahead of the host's work on the tensor maps)
       c->split_keys = may_split(pages_per_seq * c->cfg.page_size); c->attn_cluster = 1;       // the lengths themselves are on the device
@@ -2030,8 +2098,10 @@ static int attention_over_cache(tidar_ctx *c, const tidar_attention_args *x, boo
   if (!c->inflight.empty()) return fail(c, TIDAR_EINVAL, "a step is in flight");
   CacheArgs a{(const bf16 *)x->q, q_stride, x->k_pages, x->v_pages, x->n_pages, x->page_table, x->pages_per_seq, (const bf16 *)x->k_local, (const bf16 *)x->v_local, local_stride,
               (bf16 *)x->out, cf.n_q_heads, cf.n_kv_heads, WindowRows{x->seq_len, x->k, blocks, x->pages_per_seq * 64 - x->k, x->window, x->sinks}};
-  if (cf.impl == 0 && four_bits && few_rows(c, a.rows)) launch_few(c, a, x->n_seqs);
-  else {
+  if (cf.impl == 0) {
+    if (four_bits && few_rows(c, a.rows)) launch_few(c, a, x->n_seqs);
+    else if (int rc = four_bits ? launch_cache_attention<attn_tc::KV4>(c, a, x->n_seqs) : launch_cache_attention<attn_tc::WINDOW>(c, a, x->n_seqs)) return rc;
+  } else {
     Launch l(c, TIDAR_TC_ATTN);
     const dim3 grid((unsigned)R, cf.n_q_heads);
     const float scale = 1.0f / sqrtf((float)cf.head_dim);

@@ -241,6 +241,33 @@ def test_causal_chunks(impl, kv4, hd, Hq, Hkv):
     t.close()
 
 
+def _lengths(rng, n_seqs, longest):
+    ns = [int(x) for x in rng.integers(0, 130, n_seqs)]
+    ns[n_seqs // 2], ns[1] = longest, -1
+    return ns
+
+
+@pytest.mark.parametrize("kv4", [True, False])
+@pytest.mark.parametrize("n_seqs,k,blocks,longest,window,sinks", [
+    (40, 8, True, 900, 0, 0),             # more tiles than SMs, few pages: two CTAs per SM where pages are loaded whole
+    (40, 8, True, 2700, 0, 0),            # ... many pages: planned
+    (40, 8, True, 2700, 500, 70),         # ... within a window
+    (60, 5, True, 3000, 0, 0),            # tiles of ragged lengths, cut key ranges
+    (6, 16, True, 4000, 0, 0),
+    (280, 5, True, 500, 100, 1),          # more units than are planned
+    (300, 1, False, 700, 0, 0),
+    (2, 70, False, 2600, 0, 0),           # two sequences' causal rows
+    (1, 16, True, 3500, 0, 0),            # cut evenly
+    (1, 16, True, 3500, 2000, 4)])
+def test_ways_to_distribute_work(kv4, n_seqs, k, blocks, longest, window, sinks):
+    hd, Hq, Hkv = 64, 4, 2
+    t = H.lib_context(hd, Hq, Hkv, n_seqs * k * (k + 1 if blocks else 1))
+    rng = np.random.default_rng(n_seqs + k)
+    ns = _lengths(rng, n_seqs, longest) if n_seqs > 2 else [longest] + [longest // 3] * (n_seqs - 1)
+    _attention_case(t, kv4, hd, Hq, Hkv, k, blocks, ns, window, sinks, 35 + n_seqs)
+    t.close()
+
+
 @pytest.mark.parametrize("impl", IMPLS)
 @pytest.mark.parametrize("kv4", [True, False])
 def test_absent_sequences_and_pages_outside_the_pool(impl, kv4):
