@@ -10,6 +10,7 @@ CPU or PyTorch fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import List, Optional, Sequence
 
@@ -410,23 +411,37 @@ class Tidar:
 
     # -- a paged cache that the caller keeps -----------------------------------
     def _tensor(self, name, x, dtype, shape, row_strided=False):
-        """Checks a caller's tensor (its device, type, shape, layout) and returns its address; a None in `shape` stands for any size."""
+        """Checks a caller's tensor (its device, type, shape, layout) and returns its address."""
+        if isinstance(x, torch.Tensor) and x.dtype is dtype and x.get_device() == self._device_index() and x.shape == shape and x.is_contiguous():
+            return x.data_ptr()
         if not isinstance(x, torch.Tensor):
             raise ValueError(f"{name} must be a tensor")
-        if x.device.type != "cuda" or (self.device.index is not None and x.device.index != self.device.index):
+        if x.get_device() != self._device_index():
             raise ValueError(f"{name} is on {x.device}, the context on {self.device}")
         if x.dtype != dtype:
             raise ValueError(f"{name} must be {dtype}, not {x.dtype}")
-        if x.dim() != len(shape) or any(b is not None and a != b for a, b in zip(x.shape, shape)):
-            raise ValueError(f"{name} must have shape {tuple('any' if b is None else b for b in shape)}, not {tuple(x.shape)}")
-        inner = x[0] if row_strided and x.shape[0] else x
-        if not inner.is_contiguous() or (row_strided and x.shape[0] > 1 and x.stride(0) < inner.numel()):
+        if x.shape != shape:
+            raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(x.shape)}")
+        if not row_strided or not x[0].is_contiguous() or (x.shape[0] > 1 and x.stride(0) < x[0].numel()):
             raise ValueError(f"{name} must be contiguous" + (" within a row, its rows apart" if row_strided else ""))
         return x.data_ptr()
 
+    def _device_index(self):
+        return self.device.index if self.device.index is not None else torch.cuda.current_device()
+
+    def _on_device(self, entry, *args):
+        """Calls a library entry with the context's device current."""
+        if torch.cuda.current_device() == self._device_index():
+            self._check(entry(self.ctx, *args))
+        else:
+            with torch.cuda.device(self.device):
+                self._check(entry(self.ctx, *args))
+
     @staticmethod
-    def _row_stride(x):
-        return x.stride(0) if x.shape[0] > 1 else x[0].numel() if x.shape[0] else x.shape[1] * x.shape[2]
+    def _length(name, x, dim=0):
+        if not isinstance(x, torch.Tensor) or x.dim() <= dim:
+            raise ValueError(f"{name} must be a tensor of at least {dim + 1} dimensions")
+        return x.shape[dim]
 
     def page_map(self, seq_len, n_new, held, free_pages, page_table, held_out, row_start, slots, counts, free_begin=None):
         """Page table entries and slots for the rows that sequences are about to get (see tidar_page_map).
@@ -434,54 +449,49 @@ class Tidar:
         int32 device tensors: ``seq_len``, ``n_new``, ``held``, ``held_out`` [n_seqs], ``free_pages`` [n_free], ``page_table``
         [n_seqs, pages_per_seq], ``row_start`` [n_seqs + 1], ``slots`` [max_rows], ``counts`` [3], ``free_begin`` [1] or None
         (``counts[:1]`` of the call before)."""
-        i32, B = torch.int32, seq_len.shape[0]
-        p = {n: self._tensor(n, x, i32, sh) for n, x, sh in (
-            ("seq_len", seq_len, (B,)), ("n_new", n_new, (B,)), ("held", held, (B,)), ("free_pages", free_pages, (None,)), ("page_table", page_table, (B, None)),
-            ("held_out", held_out, (B,)), ("row_start", row_start, (B + 1,)), ("slots", slots, (None,)), ("counts", counts, (3,)))}
-        begin = None if free_begin is None else self._tensor("free_begin", free_begin, i32, (1,))
-        with torch.cuda.device(self.device):
-            self._check(self.lib.tidar_page_map(self.ctx, p["seq_len"], p["n_new"], p["held"], B, p["free_pages"], free_pages.shape[0], begin, p["page_table"],
-                                                page_table.shape[1], p["held_out"], p["row_start"], p["slots"], slots.shape[0], p["counts"]))
+        i32, tensor, n = torch.int32, self._tensor, self._length("seq_len", seq_len)
+        one, n_free, width, rows = (n,), self._length("free_pages", free_pages), self._length("page_table", page_table, 1), self._length("slots", slots)
+        self._on_device(self.lib.tidar_page_map, tensor("seq_len", seq_len, i32, one), tensor("n_new", n_new, i32, one), tensor("held", held, i32, one), n,
+                        tensor("free_pages", free_pages, i32, (n_free,)), n_free, None if free_begin is None else tensor("free_begin", free_begin, i32, (1,)),
+                        tensor("page_table", page_table, i32, (n, width)), width, tensor("held_out", held_out, i32, one), tensor("row_start", row_start, i32, (n + 1,)),
+                        tensor("slots", slots, i32, (rows,)), rows, tensor("counts", counts, i32, (3,)))
 
     def _kv4_rows(self, k, v, slots, k_pages, v_pages):
-        hkv, hd, rows = self.shape.n_kv_heads, self.shape.head_dim, slots.shape[0]
-        pool = (k_pages.shape[0], hkv, kv4_page_bytes(hd))
-        return (self._tensor("k", k, torch.bfloat16, (rows, hkv, hd), True), self._row_stride(k), self._tensor("v", v, torch.bfloat16, (rows, hkv, hd), True), self._row_stride(v),
-                self._tensor("slots", slots, torch.int32, (rows,)), rows, self._tensor("k_pages", k_pages, torch.uint8, pool), self._tensor("v_pages", v_pages, torch.uint8, pool), pool[0])
+        hkv, hd, rows, n_pages = self.shape.n_kv_heads, self.shape.head_dim, self._length("slots", slots), self._length("k_pages", k_pages)
+        shape, pool = (rows, hkv, hd), (n_pages, hkv, kv4_page_bytes(hd))
+        return (self._tensor("k", k, torch.bfloat16, shape, True), self._tensor("v", v, torch.bfloat16, shape, True), self._tensor("slots", slots, torch.int32, (rows,)),
+                self._tensor("k_pages", k_pages, torch.uint8, pool), self._tensor("v_pages", v_pages, torch.uint8, pool), rows, n_pages,
+                k.stride(0) if rows > 1 else hkv * hd, v.stride(0) if rows > 1 else hkv * hd)
 
     def kv4_store(self, k, v, slots, k_pages, v_pages):
         """Rows of K and V [rows, n_kv_heads, head_dim] (rows may be strided) into 4-bit pages (see tidar_kv4_store)."""
-        pk, sk, pv, sv, ps, rows, kp, vp, n = self._kv4_rows(k, v, slots, k_pages, v_pages)
-        if rows == 0:
-            return
-        with torch.cuda.device(self.device):
-            self._check(self.lib.tidar_kv4_store(self.ctx, pk, sk, pv, sv, ps, rows, kp, vp, n))
+        pk, pv, ps, kp, vp, rows, n_pages, sk, sv = self._kv4_rows(k, v, slots, k_pages, v_pages)
+        if rows:
+            self._on_device(self.lib.tidar_kv4_store, pk, sk, pv, sv, ps, rows, kp, vp, n_pages)
 
     def kv4_load(self, k_pages, v_pages, slots, k, v):
         """The values that slots of 4-bit pages stand for, into rows of K and V (see tidar_kv4_load)."""
-        pk, sk, pv, sv, ps, rows, kp, vp, n = self._kv4_rows(k, v, slots, k_pages, v_pages)
-        if rows == 0:
-            return
-        with torch.cuda.device(self.device):
-            self._check(self.lib.tidar_kv4_load(self.ctx, kp, vp, n, ps, rows, pk, sk, pv, sv))
+        pk, pv, ps, kp, vp, rows, n_pages, sk, sv = self._kv4_rows(k, v, slots, k_pages, v_pages)
+        if rows:
+            self._on_device(self.lib.tidar_kv4_load, kp, vp, n_pages, ps, rows, pk, sk, pv, sv)
 
     def _attention_cache(self, entry, record, dtype, q, k_pages, v_pages, page_table, seq_len, k_local, v_local, out, n_seqs, k, window, sinks):
-        hq, hkv, hd = self.shape.n_q_heads, self.shape.n_kv_heads, self.shape.head_dim
+        hq, hkv, hd, bf16, tensor = self.shape.n_q_heads, self.shape.n_kv_heads, self.shape.head_dim, torch.bfloat16, self._tensor
         blocks = k_local is not None or v_local is not None
-        rows, n_pages = n_seqs * k * (k + 1 if blocks else 1), k_pages.shape[0]
-        a = tidar_attention_args(
-            q=self._tensor("q", q, torch.bfloat16, (rows, hq, hd), True), q_stride=self._row_stride(q),
-            k_pages=self._tensor("k_pages", k_pages, dtype, (n_pages, hkv) + record), v_pages=self._tensor("v_pages", v_pages, dtype, (n_pages, hkv) + record), n_pages=n_pages,
-            page_table=self._tensor("page_table", page_table, torch.int32, (n_seqs, None)), pages_per_seq=page_table.shape[1],
-            seq_len=self._tensor("seq_len", seq_len, torch.int32, (n_seqs,)), out=self._tensor("out", out, torch.bfloat16, (rows, hq * hd)),
-            n_seqs=n_seqs, k=k, window=window, sinks=sinks)
+        rows, n_pages, width = n_seqs * k * (k + 1 if blocks else 1), self._length("k_pages", k_pages), self._length("page_table", page_table, 1)
+        pool = (n_pages, hkv) + record
+        pkl = pvl = None
+        local_stride = 0
         if blocks:
-            a.k_local, a.v_local = (self._tensor(n, x, torch.bfloat16, (n_seqs * k * k, hkv, hd), True) for n, x in (("k_local", k_local), ("v_local", v_local)))
-            a.local_stride = self._row_stride(k_local)
-            if self._row_stride(v_local) != a.local_stride:
+            shape = (n_seqs * k * k, hkv, hd)
+            pkl, pvl = tensor("k_local", k_local, bf16, shape, True), tensor("v_local", v_local, bf16, shape, True)
+            local_stride = k_local.stride(0) if shape[0] > 1 else 0
+            if shape[0] > 1 and v_local.stride(0) != local_stride:
                 raise ValueError("k_local and v_local must have the same row stride")
-        with torch.cuda.device(self.device):
-            self._check(entry(self.ctx, C.byref(a)))
+        args = tidar_attention_args(tensor("q", q, bf16, (rows, hq, hd), True), q.stride(0) if rows > 1 else 0, tensor("k_pages", k_pages, dtype, pool), tensor("v_pages", v_pages, dtype, pool),
+                                    n_pages, tensor("page_table", page_table, torch.int32, (n_seqs, width)), width, tensor("seq_len", seq_len, torch.int32, (n_seqs,)), pkl, pvl,
+                                    local_stride, tensor("out", out, bf16, (rows, hq * hd)), n_seqs, k, window, sinks)
+        self._on_device(entry, C.byref(args))
 
     def attention_kv4(self, q, k_pages, v_pages, page_table, seq_len, k_local, v_local, out, n_seqs: int, k: int, window: int = 0, sinks: int = 0):
         """Attention over 4-bit pages, of a step (with local rows) or of causal rows alone (k_local = v_local = None; k = 1: one token
@@ -495,6 +505,7 @@ class Tidar:
                               k_local, v_local, out, n_seqs, k, window, sinks)
 
 
+@functools.lru_cache(maxsize=None)
 def kv4_page_bytes(head_dim: int) -> int:
     """Bytes of one page of one KV head in 4 bits (see tidar_kv4_page_bytes)."""
     n = C.c_size_t(0)

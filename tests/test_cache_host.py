@@ -28,7 +28,7 @@ def test_calls_without_a_context_are_refused():
 def test_the_binding_refuses_tensors_of_another_device_type_or_shape():
     t = Tidar.__new__(Tidar)
     t.device = torch.device("cuda:0")
-    for x in (torch.zeros(3), None, [1, 2]):
+    for x in (torch.zeros(3), torch.zeros(3, dtype=torch.int32), None, [1, 2]):
         with pytest.raises(ValueError):
             t._tensor("x", x, torch.float32, (3,))
 
