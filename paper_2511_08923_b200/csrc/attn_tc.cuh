@@ -58,9 +58,9 @@ namespace attn_tc {
 
 constexpr int PAGE = 64;             // keys per step (= page size)
 // warp 0: K loads, 1: MMA, 2: watcher, 3: Q and V loads; warps 4..7 / 8..11: softmax of stream A / B
-// (KV4: and four more, which turn codes into operand tiles)
+// (KV4: and eight more, which turn codes into operand tiles)
 enum { PLAIN = 0, WINDOW = 1, KV4 = 2 };       // CACHE: the library's pages and tidar_attention's; a caller's pages within a window, bf16; the same in 4 bits
-__host__ __device__ constexpr int threads(int streams, int cache = PLAIN) { return 128 + 128 * streams + (cache == KV4 ? 128 : 0); }
+__host__ __device__ constexpr int threads(int streams, int cache = PLAIN) { return 128 + 128 * streams + (cache == KV4 ? 256 : 0); }
 constexpr int MAX_SPLITS = 32;       // items per tile
 constexpr int MAX_CLUSTER = 8;       // CTAs that may share an item
 constexpr int SLOTS_PER_SM = 2;      // partial results that fit the scratch = grid of a pass whose key ranges may be split
@@ -122,9 +122,11 @@ struct Args {
 
 // Shared memory of one CTA; everything is dynamic so that the 1024-byte alignment the
 // swizzled tiles need costs no padding (the kernel checks the base address).
-template <int HD, int STREAMS = 2, bool CLUSTER = false>
+template <int HD, int STREAMS = 2, bool CLUSTER = false, bool CODES = false>
 struct Smem {
-  static constexpr int K_STAGES = CLUSTER ? 4 : STREAMS == 2 ? 5 : 3, V_STAGES = CLUSTER ? 3 : STREAMS == 2 ? 5 : 2;     // pages in flight (one stream: two CTAs fit an SM)
+  // pages in flight (one stream: two CTAs fit an SM)
+  static constexpr int K_STAGES = CODES || CLUSTER ? 4 : STREAMS == 2 ? 5 : 3, V_STAGES = CODES ? (CLUSTER ? 2 : 4) : CLUSTER ? 3 : STREAMS == 2 ? 5 : 2;
+  static constexpr int CODE_STAGES = CODES ? (CLUSTER ? 2 : 3) : 0, RECORD = CODES ? kv4::record_bytes(HD) : 0;      // 4-bit pages on their way to the tiles
   static constexpr int NH = HD / 64;                 // 64-element halves of a head
   static constexpr int Q_BYTES = 128 * HD * 2;       // one query tile
   static constexpr int KV_BYTES = PAGE * HD * 2;
@@ -134,7 +136,8 @@ struct Smem {
   // CLUSTER: this CTA's columns of the tile's result as every CTA of the cluster has them, [CTA][stream][columns / 4][128 rows][4] floats, and
   // the CTAs' (reference max, sum), [CTA][128 rows].  (Written by the others at any time, hence a place of its own.)
   static constexpr int PEER_OFF = V_OFF + V_STAGES * KV_BYTES, PEER_ML_OFF = PEER_OFF + (CLUSTER ? 128 * HD * 4 : 0);
-  static constexpr int BAR_OFF = PEER_ML_OFF + (CLUSTER ? MAX_CLUSTER * 128 * 8 : 0);    // mbarriers and a few words
+  static constexpr int CODE_OFF = PEER_ML_OFF + (CLUSTER ? MAX_CLUSTER * 128 * 8 : 0);   // [stage][K, V] records
+  static constexpr int BAR_OFF = CODE_OFF + CODE_STAGES * 2 * RECORD;                    // mbarriers and a few words
   static constexpr int TOTAL = BAR_OFF + 512;
   static constexpr int XCHG_OFF = K_OFF;             // single tile: the streams' results, [stream][hd / 8][128 rows][4] floats; (max, sum) behind them
   static constexpr int XCHG_ML_OFF = XCHG_OFF + 128 * HD * 4;
@@ -142,10 +145,15 @@ struct Smem {
 };
 static_assert(Smem<128, 2, true>::XCHG_ML_OFF + 2 * 128 * 8 <= Smem<128, 2, true>::PEER_OFF && Smem<64, 2, true>::XCHG_ML_OFF + 2 * 128 * 8 <= Smem<64, 2, true>::PEER_OFF &&
               Smem<128, 2, true>::TOTAL <= 227 * 1024, "exchange area fits the K/V rings of a cluster's CTA");
+static_assert(Smem<128, 2, true, true>::XCHG_ML_OFF + 2 * 128 * 8 <= Smem<128, 2, true, true>::PEER_OFF && Smem<64, 2, true, true>::XCHG_ML_OFF + 2 * 128 * 8 <= Smem<64, 2, true, true>::PEER_OFF &&
+              Smem<128, 2, true, true>::TOTAL <= 227 * 1024 && Smem<128, 2, false, true>::TOTAL <= 227 * 1024 && Smem<64, 2, false, true>::XCHG_ML_OFF + 2 * 128 * 8 <= Smem<64, 2, false, true>::BAR_OFF,
+              "4-bit pages: the same");
 static_assert(Smem<128>::XCHG_ML_OFF + 2 * 128 * 8 <= Smem<128>::BAR_OFF && Smem<64>::XCHG_ML_OFF + 2 * 128 * 8 <= Smem<64>::BAR_OFF, "exchange area fits the K/V rings");
 
 struct Ctl {                                         // lives at Smem::BAR_OFF
   uint64_t q_full, k_full[5], k_empty[5], v_full[5], v_empty[5], s_full[2][2], p_full[2][2];
+  uint64_t code_full[5], code_empty[5];              // KV4: a turn's records of K and V
+  int code_live[2][5];                               // [K, V]: whether the record was loaded (0: its page is not in the pool)
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -177,9 +185,13 @@ constexpr int CAND = 32;                               // limits tried per pairi
 // The estimate, for the plan kernel and for the host, which decides with it whether a step's merge kernel is needed at all (step_attention): limit number i
 // of the units or tiles the longest of which takes `longest` us; pieces of an entity of `us` us, at most one per page; what all entities come to.
 struct PlanCost { int items, live, most; float sum, longest; };
+// 4-bit pages (CODES) cost a single tile more: its turn is as long as the warps that fill the tiles take, which in a pair two tiles share.
+constexpr float CODES_PAIR_PAGE = 1.3f, CODES_SINGLE_PAGE = 0.92f;
+template <bool CODES> __host__ __device__ constexpr float page_us(bool pair) { return CODES ? (pair ? CODES_PAIR_PAGE : CODES_SINGLE_PAGE) : pair ? PAIR_PAGE : SINGLE_PAGE; }
 __host__ __device__ inline float plan_limit(float longest, int i) { return fmaxf(longest / (1.f + 0.5f * i), 0.1f) * 1.0001f; }
+template <bool CODES = false>
 __host__ __device__ inline int plan_pieces(float us, float limit, bool dbl) {
-  const float n = us / limit, pages = us * (dbl ? 1.0001f / PAIR_PAGE : 1.0001f / SINGLE_PAGE);
+  const float n = us / limit, pages = us * (dbl ? 1.0001f / page_us<CODES>(true) : 1.0001f / page_us<CODES>(false));
 #ifdef __CUDA_ARCH__
   return (int)fminf(ceilf(n), pages);
 #else
@@ -187,8 +199,9 @@ __host__ __device__ inline int plan_pieces(float us, float limit, bool dbl) {
   return std::min(up, (int)pages);
 #endif
 }
+template <bool CODES = false>
 __host__ __device__ inline void plan_add(PlanCost &c, float us, float limit, bool dbl, int times = 1) {
-  const int k = plan_pieces(us, limit, dbl);
+  const int k = plan_pieces<CODES>(us, limit, dbl);
   const float store = k > 1 ? (dbl ? PAIR_STORE : SINGLE_STORE) : 0.f;
 #ifdef __CUDA_ARCH__
   const float piece = __fdividef(us, (float)k);
@@ -197,7 +210,7 @@ __host__ __device__ inline void plan_add(PlanCost &c, float us, float limit, boo
 #endif
   c.items += times * k; c.live += times; c.most = k > c.most ? k : c.most;
   c.sum += times * (us + k * (OVERHEAD + store));
-  c.longest = fmaxf(c.longest, piece + (k > 1 ? 0.5f * SINGLE_PAGE : 0.f) + store + OVERHEAD);
+  c.longest = fmaxf(c.longest, piece + (k > 1 ? 0.5f * page_us<CODES>(false) : 0.f) + store + OVERHEAD);
 }
 __host__ __device__ inline float plan_time(const PlanCost &c, int Hkv, int n_sms) {
   float us = c.longest;
@@ -212,7 +225,7 @@ struct RowKeys { int nvis, loc0, nloc, seq; };
 __device__ __forceinline__ int skipped_pages(int low, int n_cache, int sink_pages) { return max(min(low / PAGE, n_cache) - sink_pages, 0); }
 static_assert(sizeof(RowKeys) != sizeof(WindowKeys), "plan_block tells them apart by size");
 
-template <typename ROW>
+template <bool CODES = false, typename ROW>
 __device__ inline void plan_block(const PlanArgs &p, ROW row_keys) {
   constexpr bool WINDOWED = sizeof(row_keys(0)) == sizeof(WindowKeys);
   struct Keys { int n_cache, n_pages, loc_lo, skip; }; // (a sequence of more than 32767 pages fits a B200)
@@ -261,7 +274,7 @@ __device__ inline void plan_block(const PlanArgs &p, ROW row_keys) {
       const int n_pages = n_cache + (h > l ? (h - l + PAGE - 1) / PAGE : 0);
       if (planned) {
         keys[lane][u] = Keys{n_cache, n_pages, l, skip};
-        const float us = n_pages * (lane == 2 && two ? PAIR_PAGE : SINGLE_PAGE);
+        const float us = n_pages * page_us<CODES>(lane == 2 && two);
         ent_us[lane == 2 ? u : p.n_units + 2 * u + lane] = us;
         atomicMax(&longest_us[lane == 2 ? 0 : 1], __float_as_int(us));
         if (lane == 0) { unit_row0[u] = row0; unit_rend[u] = row_end; unit_seq[u] = seq; }
@@ -286,7 +299,7 @@ __device__ inline void plan_block(const PlanArgs &p, ROW row_keys) {
     PlanCost cost{0, 0, 0, 0.f, 0.f};
     for (int e = sub; e < n_ent; e += per) {
       const float us = ent_us[e0 + e];
-      if (us > 0.f) plan_add(cost, us, lim, pr && unit_row0[e] + p.spt < unit_rend[e]);
+      if (us > 0.f) plan_add<CODES>(cost, us, lim, pr && unit_row0[e] + p.spt < unit_rend[e]);
     }
     for (int o = per >> 1; o > 0; o >>= 1) {
       cost.items += __shfl_xor_sync(0xffffffffu, cost.items, o); cost.live += __shfl_xor_sync(0xffffffffu, cost.live, o);
@@ -308,7 +321,7 @@ __device__ inline void plan_block(const PlanArgs &p, ROW row_keys) {
   const int n_ent = paired ? p.n_units : 2 * p.n_units, e0 = paired ? 0 : p.n_units;
   for (int e = threadIdx.x; e < n_ent; e += blockDim.x) {
     const float us = ent_us[e0 + e];
-    const int k = us <= 0.f ? 0 : splits ? max(1, plan_pieces(us, limit, paired && unit_row0[e] + p.spt < unit_rend[e])) : 1;
+    const int k = us <= 0.f ? 0 : splits ? max(1, plan_pieces<CODES>(us, limit, paired && unit_row0[e] + p.spt < unit_rend[e])) : 1;
     ent_n[e] = (short)k; ent_us[e0 + e] = k ? us / k : -1.f;
   }
   __syncthreads();
@@ -472,14 +485,13 @@ __device__ __noinline__ void finish_alone(uint32_t o_addr, int t, int my_row, fl
 // table may lie outside the pool, and what no row sees may hold anything.  Scores of what a row does not see are replaced, so K does no harm; a weight of
 // zero times a V that is not a number would, so such rows of V are zeroed: by the watcher, in the few pages that have any (WINDOW, and local rows), before it
 // releases their product.
-//   KV4: four more warps take the place of the page loads: each thread holds the codes of a row's half head, loaded two pages ahead straight from
-//   global memory, and stores them as bf16 in the layout a TMA load would have given them.  16 K elements of K and V per page cost 128 threads about
-//   250 instructions each; what a page of 1 us (pair) or 0.56 us (single) leaves idle.
+//   KV4: the load warps bring records of codes, and eight more warps turn them into bf16 tiles in the layout that a TMA load would have given.  A page's
+//   16 K elements of K and V cost them 130 instructions each.
 template <int HD, int STREAMS, bool DIRECT, bool AHEAD, bool CLUSTER, int CACHE>
 __global__ void __launch_bounds__(threads(STREAMS, CACHE), 3 - STREAMS)
 attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                const __grid_constant__ CUtensorMap tmKloc, const __grid_constant__ CUtensorMap tmVloc, const Args a, const TlSlot tl) {
-  using L = Smem<HD, STREAMS, CLUSTER>;
+  using L = Smem<HD, STREAMS, CLUSTER, CACHE == KV4>;
   constexpr int NH = L::NH;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const int warp = sm100::warp_index(), lane = threadIdx.x & 31;
@@ -495,9 +507,11 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
   if (threadIdx.x == 0) {
     ctl.abort_flag = 0;
     sm100::mbar_init(sm100::smem_u32(&ctl.q_full), 1);
-    constexpr int FILLERS = CACHE == KV4 ? 4 : 1;      // warps, or the one thread that issues a load
+    constexpr int FILLERS = CACHE == KV4 ? HD / 16 : 1;      // warps, or the one thread that issues a load
     for (int s = 0; s < L::K_STAGES; ++s) { sm100::mbar_init(sm100::smem_u32(&ctl.k_full[s]), FILLERS); sm100::mbar_init(sm100::smem_u32(&ctl.k_empty[s]), 1); }
     for (int s = 0; s < L::V_STAGES; ++s) { sm100::mbar_init(sm100::smem_u32(&ctl.v_full[s]), FILLERS); sm100::mbar_init(sm100::smem_u32(&ctl.v_empty[s]), 1); }
+    if constexpr (CACHE == KV4)
+      for (int i = 0; i < L::CODE_STAGES; ++i) { sm100::mbar_init(sm100::smem_u32(&ctl.code_full[i]), 2); sm100::mbar_init(sm100::smem_u32(&ctl.code_empty[i]), 8); }
     for (int t = 0; t < STREAMS; ++t)
       for (int b = 0; b < 2; ++b) { sm100::mbar_init(sm100::smem_u32(&ctl.s_full[t][b]), 1); sm100::mbar_init(sm100::smem_u32(&ctl.p_full[t][b]), 4); }
     sm100::fence_mbar_init();
@@ -543,6 +557,9 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
   const int my_row = (warp & 3) * 32 + lane;             // and this thread's MMA row = TMEM lane
   int my_slot = -1;                                      // and its slot, -1: none
   const int c_cols = (HD / 2) >> c_log, c_shift = 31 - __clz(c_cols);     // columns of a stream's half that a CTA of the cluster finishes (at least 8)
+  // KV4: the softmax warps take over registers of the others: 256 x 128 + 384 x 72 of the 640 x 96 that the block was launched with.
+  if (warp < 4) {
+  if constexpr (CACHE == KV4) sm100::setmaxnreg_dec<72>();
   if (warp == 0 || warp == 3) {
     // ===================== K producer / Q and V producer =====================
     // Lane i holds the i-th entry of a group of 32 entries of the page table, so that a page's load does not wait for
@@ -575,7 +592,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
           }
           __syncwarp();
         }
-        if (p == np || CACHE == KV4) break;              // (KV4: pages have warps of their own)
+        if (p == np || CACHE == KV4) break;              // (KV4: see below)
         if ((p & 31) == 0) {
           if (p) cur = next;
           next = p + 32 + lane < n_table ? table[table_at(p_begin + p + 32 + lane)] : 0;
@@ -590,6 +607,34 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         }
         __syncwarp();
         if (++s == stages) { s = 0; ph ^= 1u; }
+      }
+      if constexpr (CACHE == KV4) {
+        // Records for the warps that fill the tiles: K of page i and V of page i - lead make up turn i (local rows those warps load themselves).
+        const int lead = min(ahead, np), which = is_k ? 0 : 1, first = is_k ? 0 : lead;
+        int c = 0; uint32_t cp = 1u;
+        for (int i = 0; n_table > 0 && i < n_table + lead; ++i) {
+          const int p = i - first;
+          int page = -1;
+          if (p >= 0 && p < n_table) {
+            if ((p & 31) == 0) {
+              if (p) cur = next;
+              next = p + 32 + lane < n_table ? table[table_at(p_begin + p + 32 + lane)] : 0;
+            }
+            page = __shfl_sync(0xffffffffu, cur, p & 31);
+          }
+          if (!sm100::mbar_wait_warp(sm100::smem_u32(&ctl.code_empty[c]), cp, abortp)) break;
+          if (sm100::elect_one()) {
+            const uint32_t fb = sm100::smem_u32(&ctl.code_full[c]);
+            const bool live = (unsigned)page < (unsigned)a.win.n_pages;
+            ctl.code_live[which][c] = live;
+            if (live) {
+              sm100::mbar_expect_tx(fb, (uint32_t)L::RECORD);
+              sm100::bulk_load(smem0 + L::CODE_OFF + (uint32_t)((c * 2 + which) * L::RECORD), (is_k ? a.win.k4 : a.win.v4) + ((size_t)page * a.Hkv + kvh) * L::RECORD, (uint32_t)L::RECORD, fb);
+            } else sm100::mbar_arrive(fb);
+          }
+          __syncwarp();
+          if (++c == L::CODE_STAGES) { c = 0; cp ^= 1u; }
+        }
       }
     }
   } else if (warp == 1) {
@@ -648,7 +693,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       if (++sv == L::V_STAGES) sv = 0;
       if (++sk == L::K_STAGES) sk = 0;
     }
-  } else if (warp == 2) {
+  } else {
     // ===================== watcher =====================
     // Waits (bounded) for what each group of MMAs needs and arrives on the group's hardware barrier.  A barrier
     // cannot be arrived on twice before the MMA warp has passed it: P of step j + 2 needs the scores whose products
@@ -656,20 +701,22 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
     // meets the MMA warp at every barrier instead.
     bool failed = false;
     // Rows of a V page that no row of the call sees become zeros: positions behind the sequence's causal slots, those between the sinks and the window of its
-    // first slot, and local rows behind the sequence's own.
-    auto clear_unseen = [&](int p, uint32_t tile) {
-      const WindowRows &w = a.win.rows;
-      const int n = min(w.seq_len[item.seq], w.n_max), l = p_begin + p;
-      int from, gap0 = 0, gap1 = 0;                      // rows [gap0, gap1) and from `from` on
-      if (l < item.n_cache_pages) {
-        if constexpr (CACHE == KV4) return;              // (zeroed where the codes are read)
+    // first slot, and local rows behind the sequence's own.  Which rows of page p these are, [gap0, gap1) and from `from` on, is known ahead of the page.
+    const WindowRows &w = a.win.rows;
+    const int n = CACHE == WINDOW && np > 0 ? min(w.seq_len[item.seq], w.n_max) : 0;
+    int from = PAGE, gap0 = 0, gap1 = 0;
+    auto find_unseen = [&](int p) {
+      const int l = p_begin + p;
+      from = PAGE; gap0 = gap1 = 0;
+      if (l >= item.n_cache_pages) from = (item.seq + 1) * w.k * w.k - (item.loc_lo + (l - item.n_cache_pages) * PAGE);
+      else if (CACHE == WINDOW) {                        // (KV4: zeroed where the codes are read)
         const int pos = table_at(l) * PAGE;
         from = n + w.k - pos;
-        if (w.window > 0) { gap0 = w.sinks - pos; gap1 = n - w.window + 1 - pos; }
-      } else {
-        from = (item.seq + 1) * w.k * w.k - (item.loc_lo + (l - item.n_cache_pages) * PAGE);
+        if (w.window > 0) { gap0 = max(w.sinks - pos, 0); gap1 = min(n - w.window + 1 - pos, PAGE); }
       }
-      if (from >= PAGE && (gap1 <= 0 || gap0 >= PAGE || gap0 >= gap1)) return;
+      return from < PAGE || gap0 < gap1;
+    };
+    auto clear_unseen = [&](uint32_t tile) {
       for (int i = lane; i < PAGE * NH * 8; i += 32) {
         const int row = i >> 3 & (PAGE - 1);
         if (row >= from || (row >= gap0 && row < gap1)) sm100::st_shared_zero16(tile + (uint32_t)((i >> 9) * (PAGE * 128) + (i & 511) * 16));
@@ -677,16 +724,16 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       sm100::fence_proxy_async();                        // (the product reads through the async proxy)
       __syncwarp();
     };
-    auto release = [&](uint32_t id, uint32_t bar0, uint32_t par0, uint32_t bar1, uint32_t par1, uint32_t bar2, uint32_t par2, int v_page = -1, uint32_t v_tile = 0) {
+    auto release = [&](uint32_t id, uint32_t bar0, uint32_t par0, uint32_t bar1, uint32_t par1, uint32_t bar2, uint32_t par2, uint32_t v_tile = 0) {
       if (!failed) {
         bool ok = true;
         if (lane == 0)
           ok = (!bar1 || sm100::mbar_wait(bar1, par1, abortp)) && (!bar2 || sm100::mbar_wait(bar2, par2, abortp)) && sm100::mbar_wait(bar0, par0, abortp);
         failed = !__shfl_sync(0xffffffffu, ok, 0);
         if constexpr (CACHE != PLAIN) {
-          if (v_page >= 0 && !failed) {
+          if (v_tile != 0 && !failed) {
             failed = !sm100::mbar_wait_warp(bar1, par1, abortp);       // (complete: every lane sees the load)
-            clear_unseen(v_page, v_tile);
+            clear_unseen(v_tile);
           }
         }
       }
@@ -700,13 +747,17 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       const int j = shared ? p : p >> 1, b = j & 1;
       for (int t = stream0(p); t < stream1(p); ++t) {
         const bool first_stream = !pair || t == 0;
+        uint32_t v_tile = 0;                             // the page's V, if it has rows that no row sees
+        if constexpr (CACHE != PLAIN) { if (first_stream && find_unseen(p)) v_tile = smem0 + L::V_OFF + (uint32_t)sv * L::KV_BYTES; }
         release(1u + (uint32_t)(t * 2 + b), sm100::smem_u32(&ctl.p_full[t][b]), (uint32_t)(j >> 1) & 1u, first_stream ? sm100::smem_u32(&ctl.v_full[sv]) : 0u, phv,
-                first_stream && p + ahead < np ? sm100::smem_u32(&ctl.k_full[sk]) : 0u, phk, first_stream ? p : -1, smem0 + L::V_OFF + (uint32_t)sv * L::KV_BYTES);
+                first_stream && p + ahead < np ? sm100::smem_u32(&ctl.k_full[sk]) : 0u, phk, v_tile);
       }
       if (++sv == L::V_STAGES) { sv = 0; phv ^= 1u; }
       if (++sk == L::K_STAGES) { sk = 0; phk ^= 1u; }
     }
-  } else if (warp >= 4 && warp < 4 + 4 * STREAMS) {
+  }
+  } else if (warp < 4 + 4 * STREAMS) {
+    if constexpr (CACHE == KV4) sm100::setmaxnreg_inc<128>();
     // ===================== softmax =====================
     const int tile = pair ? t : 0;
     const int nj = shared ? np : (np + 1 - t) >> 1;      // steps of this stream
@@ -928,92 +979,94 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         if (ok && !sharing) finish_alone<HD, CACHE>(o_addr, t, my_row, m_ref, l_run, nj, my_slot < 0 ? nullptr : o, xo, xml);
       }
     }
-  } else if (CACHE == KV4) {
+  } else if constexpr (CACHE == KV4) {
+    sm100::setmaxnreg_dec<72>();
     // ===================== codes to tiles =====================
-    // A thread takes the same GP groups (of 32 dimensions) of one row of every page: lanes take rows, so codes are read 512 bytes at a time, and a quarter of
-    // a warp stores to eight different banks groups of the swizzled tile.  K runs `ahead` pages in front of V, as the products do: the watcher wants K of
-    // page p + ahead before it releases P V of page p.
-    constexpr int GP = HD / 64;
-    const int tid = threadIdx.x - threads(STREAMS), row = tid & 63, group0 = (tid >> 6) * GP;
-    struct Codes { uint4 c[GP]; uint32_t sb[GP]; };
+    // A thread takes the same group (of 32 dimensions) of one row of every page, of K and V (head_dim 64: of one of them): lanes take rows, so that a warp
+    // reads codes 512 bytes at a time and a quarter of it stores to eight different bank groups of the swizzled tile.  K is `ahead` pages in front of V, as
+    // the products are (the watcher wants K of page p + ahead before it releases P V of page p): a turn is K of page i and V of page i - lead.  The products'
+    // operands keep the shared memory busy, so every access to it takes long: the codes of the next turn are read before this turn's are written.
+    constexpr bool BOTH = HD == 128;
+    const int tid = threadIdx.x - threads(STREAMS), row = tid & 63, group = (tid >> 6) & (HD / 32 - 1);
+    const bool does_k = BOTH || tid < 128, does_v = BOTH || tid >= 128;
+    const bool loads_k = tid < 32, loads_v = BOTH ? tid < 32 : tid >= 128 && tid < 160;      // the warps that load local rows
     if (np > 0) {
       const WindowRows &w = a.win.rows;
-      const int n = min(w.seq_len[item.seq], w.n_max), n_table = min(item.n_cache_pages, item.p_end) - p_begin;
-      const int32_t *table = a.page_table + (size_t)item.seq * a.pages_per_seq;
-      // the table entry of page p is fetched two pages before the codes are, which are fetched two pages before they are stored
-      auto entry = [&](int p) { return p < n_table ? __ldg(table + table_at(p_begin + p)) : -1; };
-      auto codes = [&](const uint8_t *pool, int p, int page) {
-        Codes x;
-#pragma unroll
-        for (int e = 0; e < GP; ++e) { x.c[e] = make_uint4(0, 0, 0, 0); x.sb[e] = 0; }
-        if (p < n_table && (unsigned)page < (unsigned)a.win.n_pages) {
-          const uint8_t *rec = pool + ((size_t)page * a.Hkv + kvh) * kv4::record_bytes(HD);
-          const int pos = table_at(p_begin + p) * PAGE + row;
-#pragma unroll
-          for (int e = 0; e < GP; ++e) x.c[e] = __ldg(reinterpret_cast<const uint4 *>(rec + ((group0 + e) * PAGE + row) * 16));
-          if (pos < n + w.k && (w.window == 0 || pos < w.sinks || pos > n - w.window)) {      // what no row sees stands for zeros: scale and base 0
-#pragma unroll
-            for (int e = 0; e < GP; ++e) x.sb[e] = __ldg(reinterpret_cast<const uint32_t *>(rec + kv4::code_bytes(HD) + (row * (HD / 32) + group0 + e) * 4));
-          }
+      const int n = min(w.seq_len[item.seq], w.n_max), n_table = max(min(item.n_cache_pages, item.p_end) - p_begin, 0), lead = min(ahead, np);
+      const int code_turns = n_table > 0 ? n_table + lead : 0;
+      struct Codes { uint4 c; uint32_t sb; int live; };
+      // this thread's codes of page p of K (which = 0) or V, which are in stage c (nothing read is used yet: that would wait for it)
+      auto read = [&](int p, int which, int c) {
+        Codes x{make_uint4(0u, 0u, 0u, 0u), 0u, 0};
+        if (p >= 0 && p < n_table && (which ? does_v : does_k)) {
+          const uint8_t *rec = smem_raw + L::CODE_OFF + (c * 2 + which) * L::RECORD;
+          x.c = *reinterpret_cast<const uint4 *>(rec + (group * PAGE + row) * 16);
+          x.sb = *reinterpret_cast<const uint32_t *>(rec + kv4::code_bytes(HD) + (row * (HD / 32) + group) * 4);
+          x.live = ctl.code_live[which][c];
         }
         return x;
       };
-      auto store = [&](const Codes &x, uint32_t tile) {
+      const uint32_t line = smem0 + (uint32_t)((group >> 1) * (PAGE * 128) + row * 128), chunk = (uint32_t)((((group & 1) * 4) ^ (row & 4)) << 4), flip = (uint32_t)((row & 3) << 4);
+      // page p's into its tile; what no row sees stands for zeros: scale and base 0
+      auto write = [&](const Codes &x, int p, uint32_t tile_off) {
+        const int pos = table_at(p_begin + p) * PAGE + row;
+        const uint32_t sb = x.live && pos < n + w.k && (w.window == 0 || pos < w.sinks || pos > n - w.window) ? x.sb : 0u;
+        const uint32_t ss = kv4::low_twice(sb), bb = kv4::high_twice(sb);
+        const uint32_t wd[4] = {x.c.x, x.c.y, x.c.z, x.c.w};
 #pragma unroll
-        for (int e = 0; e < GP; ++e) {
-          const uint32_t ss = kv4::low_twice(x.sb[e]), bb = kv4::high_twice(x.sb[e]);
-          const uint32_t wd[4] = {x.c[e].x, x.c[e].y, x.c[e].z, x.c[e].w};
-          const uint32_t line = tile + (uint32_t)(((group0 + e) >> 1) * (PAGE * 128) + row * 128);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t v[4];
-            kv4::values8(wd[i], ss, bb, v);
-            sm100::st_shared_v4(line + (uint32_t)(((((group0 + e) & 1) * 4 + i) ^ (row & 7)) << 4), v[0], v[1], v[2], v[3]);
-          }
+        for (int i = 0; i < 4; ++i) {
+          uint32_t v[4];
+          kv4::values8(wd[i], ss, bb, v);
+          sm100::st_shared_v4(line + tile_off + chunk + ((uint32_t)(i << 4) ^ flip), v[0], v[1], v[2], v[3]);      // 16-byte chunk 4 (group & 1) + i, swizzled
         }
-        sm100::fence_proxy_async();
-        __syncwarp();
       };
-      // one page of K or V into its stage; local rows come by TMA
-      auto fill = [&](const Codes &x, int p, bool is_k) {
-        const int stages = is_k ? L::K_STAGES : L::V_STAGES, s = p % stages;
-        const uint32_t full = sm100::smem_u32(is_k ? &ctl.k_full[s] : &ctl.v_full[s]), empty = sm100::smem_u32(is_k ? &ctl.k_empty[s] : &ctl.v_empty[s]);
-        const uint32_t tile = smem0 + (is_k ? L::K_OFF : L::V_OFF) + (uint32_t)s * L::KV_BYTES;
-        if (!sm100::mbar_wait_warp(empty, (uint32_t)(p / stages + 1) & 1u, abortp)) return false;
-        if (p < n_table) {
-          store(x, tile);
-          if (lane == 0) sm100::mbar_arrive(full);
-        } else if (tid < 32) {
+      // local rows come by TMA
+      auto load_local = [&](int p, int which, int st) {
+        if (which ? loads_v : loads_k) {
           if (sm100::elect_one()) {
+            const uint32_t full = sm100::smem_u32(which ? &ctl.v_full[st] : &ctl.k_full[st]);
             sm100::mbar_expect_tx(full, (uint32_t)L::KV_BYTES);
-            sm100::tma_load_4d(tile, is_k ? &tmKloc : &tmVloc, full, 0, item.loc_lo + (p_begin + p - item.n_cache_pages) * PAGE, 0, kvh, sm100::policy_evict_last());
+            sm100::tma_load_4d(smem0 + (which ? L::V_OFF : L::K_OFF) + (uint32_t)st * L::KV_BYTES, which ? &tmVloc : &tmKloc, full, 0,
+                               item.loc_lo + (p_begin + p - item.n_cache_pages) * PAGE, 0, kvh, sm100::policy_evict_last());
           }
           __syncwarp();
-        } else if (lane == 0) {
-          sm100::mbar_arrive(full);
         }
-        __syncwarp();
-        return true;
       };
-      pdl_wait();
-      int ke[2] = {entry(2), entry(3)}, ve[2] = {ke[0], ke[1]};
-      const int e0 = entry(0), e1 = entry(1);
-      Codes k0 = codes(a.win.k4, 0, e0), k1 = codes(a.win.k4, 1, e1), v0 = codes(a.win.v4, 0, e0), v1 = codes(a.win.v4, 1, e1);
+      // Three lanes wait for a turn's three barriers and arrive on three others, all at once (one after the other they took half of a turn's time): K's and
+      // V's tile free / full, the next turn's codes there / read.  A lane's barriers take turns in a ring, from turn `from` to `to`.
+      const uint32_t wait0 = sm100::smem_u32(lane == 0 ? ctl.k_empty : lane == 1 ? ctl.v_empty : ctl.code_full);
+      const uint32_t done0 = sm100::smem_u32(lane == 0 ? ctl.k_full : lane == 1 ? ctl.v_full : ctl.code_empty);
+      const int ring = lane == 0 ? L::K_STAGES : lane == 1 ? L::V_STAGES : L::CODE_STAGES;
+      const int from = lane == 1 ? lead : 0, to = lane == 0 ? np : lane == 1 ? np + lead : lane == 2 ? code_turns - 1 : 0;
+      const int by_load = lane == 0 && loads_k ? n_table : lane == 1 && loads_v ? n_table + lead : 0x7fffffff;      // from this turn on the load arrives for the warp that issues it
+      const bool arrives = lane == 0 ? does_k : lane == 1 ? does_v : lane == 2;
+      uint32_t st_l = lane == 2 ? 1u : 0u, par_l = lane == 2 ? 0u : 1u;
+      static_assert(L::CODE_STAGES >= 2 || CACHE != KV4, "turn 1's codes are in stage 1");
+      int sk = 0, sv = 0, c = 1;                         // the turn's stages (c: of the next one's codes)
+      Codes xk{}, xv{};
       bool ok = true;
-      auto next_k = [&](int p) {
-        ok = fill(k0, p, true);
-        k0 = k1; k1 = codes(a.win.k4, p + 2, ke[0]);
-        ke[0] = ke[1]; ke[1] = entry(p + 4);
-      };
-      auto next_v = [&](int p) {
-        ok = fill(v0, p, false);
-        v0 = v1; v1 = codes(a.win.v4, p + 2, ve[0]);
-        ve[0] = ve[1]; ve[1] = entry(p + 4);
-      };
-      for (int p = 0; ok && p < min(ahead, np); ++p) next_k(p);
-      for (int p = 0; ok && p < np; ++p) {
-        next_v(p);
-        if (ok && p + ahead < np) next_k(p + ahead);
+      if (code_turns > 0) {
+        ok = sm100::mbar_wait_warp(sm100::smem_u32(&ctl.code_full[0]), 0u, abortp);
+        xk = read(0, 0, 0); xv = read(-lead, 1, 0);
+        __syncwarp();
+        if (lane == 0) sm100::mbar_arrive(sm100::smem_u32(&ctl.code_empty[0]));
+      }
+      for (int i = 0; ok && i < np + lead; ++i) {
+        const bool mine = i >= from && i < to;
+        if (!(ok = sm100::mbar_wait_lanes(mine ? wait0 + st_l * 8u : 0u, par_l, abortp))) break;
+        const int vp = i - lead;
+        const Codes nk = read(i + 1, 0, c), nv = read(vp + 1, 1, c);
+        if (i < n_table) { if (does_k) write(xk, i, L::K_OFF + (uint32_t)sk * L::KV_BYTES); } else if (i < np) load_local(i, 0, sk);
+        if (vp >= 0) { if (vp < n_table) { if (does_v) write(xv, vp, L::V_OFF + (uint32_t)sv * L::KV_BYTES); } else load_local(vp, 1, sv); }
+        sm100::fence_proxy_async();
+        __syncwarp();
+        if (mine && arrives && i < by_load) sm100::mbar_arrive(done0 + st_l * 8u);
+        if (mine && (int)++st_l == ring) { st_l = 0; par_l ^= 1u; }
+        xk = nk; xv = nv;
+        if (++sk == L::K_STAGES) sk = 0;
+        if (vp >= 0 && ++sv == L::V_STAGES) sv = 0;
+        if (++c == L::CODE_STAGES) c = 0;
+        __syncwarp();
       }
     }
   }

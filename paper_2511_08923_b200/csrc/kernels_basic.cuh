@@ -184,10 +184,11 @@ __global__ void __launch_bounds__(512) attn_meta_plan_kernel(RowMeta m, const in
 }
 
 // The plan alone, of a call over a caller's pages (whose rows' keys follow from the lengths).
+template <bool CODES>
 __global__ void __launch_bounds__(512) attn_window_plan_kernel(WindowRows w, attn_tc::PlanArgs plan) {
   pdl_trigger();
   pdl_wait();
-  attn_tc::plan_block(plan, [&](int r) { return window_keys(w, r); });
+  attn_tc::plan_block<CODES>(plan, [&](int r) { return window_keys(w, r); });
 }
 
 // What every layer of a pass shares, computed once per pass from the row metadata: cos/sin of

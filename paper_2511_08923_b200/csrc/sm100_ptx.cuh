@@ -61,6 +61,11 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, vo
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)) != 0;
 }
 
+// Every lane waits for a barrier of its own (0: none).
+__device__ __forceinline__ bool mbar_wait_lanes(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
+  return __all_sync(0xffffffffu, bar == 0u || mbar_wait(bar, parity, abort_flag)) != 0;
+}
+
 // 2^x on the special-function unit, one instruction (denormal results flush to zero;
 // 2^-inf = 0, relative error about 2^-22).
 __device__ __forceinline__ float ex2_approx(float x) {

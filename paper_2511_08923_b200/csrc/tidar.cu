@@ -641,25 +641,23 @@ attn_tc::Args attention_args(const tidar_ctx *c, const AttnMaps &m, const KvGeom
   return a;
 }
 // One CTA per item, or (cluster > 1) a cluster of CTAs per item.
+template <int HD, int STREAMS, bool DIRECT, bool AHEAD, bool CLUSTER, int CACHE>
+void launch_attention_instance(tidar_ctx *c, int grid, int cluster, const AttnMaps &m, const attn_tc::Args &a, TlSlot tl) {
+  launch_pdl_cluster(cluster, attn_tc::attn_tc_kernel<HD, STREAMS, DIRECT, AHEAD, CLUSTER, CACHE>, grid * cluster, attn_tc::threads(STREAMS, CACHE),
+                     attn_tc::Smem<HD, STREAMS, CLUSTER, CACHE == attn_tc::KV4>::TOTAL, c->stream, *m.q, *m.k, *m.v, *m.kloc, *m.vloc, a, tl);
+}
 template <int STREAMS, bool DIRECT, bool AHEAD = false, int CACHE = attn_tc::PLAIN>
 void launch_attention_kernel(tidar_ctx *c, int grid, const AttnMaps &m, const attn_tc::Args &a, int cluster = 1) {
   Launch l(c, TIDAR_TC_ATTN);
-  const int threads = attn_tc::threads(STREAMS, CACHE);
   if constexpr (STREAMS == 2 && (DIRECT || CACHE == attn_tc::PLAIN)) {      // (calls over a caller's pages share items only where they have no plan)
     if (cluster > 1) {
-      if (c->cfg.head_dim == 128)
-        launch_pdl_cluster(cluster, attn_tc::attn_tc_kernel<128, 2, DIRECT, AHEAD, true, CACHE>, grid * cluster, threads, attn_tc::Smem<128, 2, true>::TOTAL, c->stream, *m.q, *m.k,
-                           *m.v, *m.kloc, *m.vloc, a, l.tl);
-      else
-        launch_pdl_cluster(cluster, attn_tc::attn_tc_kernel<64, 2, DIRECT, AHEAD, true, CACHE>, grid * cluster, threads, attn_tc::Smem<64, 2, true>::TOTAL, c->stream, *m.q, *m.k,
-                           *m.v, *m.kloc, *m.vloc, a, l.tl);
+      if (c->cfg.head_dim == 128) launch_attention_instance<128, 2, DIRECT, AHEAD, true, CACHE>(c, grid, cluster, m, a, l.tl);
+      else launch_attention_instance<64, 2, DIRECT, AHEAD, true, CACHE>(c, grid, cluster, m, a, l.tl);
       return;
     }
   }
-  if (c->cfg.head_dim == 128)
-    launch_pdl(attn_tc::attn_tc_kernel<128, STREAMS, DIRECT, AHEAD, false, CACHE>, grid, threads, attn_tc::Smem<128, STREAMS>::TOTAL, c->stream, *m.q, *m.k, *m.v, *m.kloc, *m.vloc, a, l.tl);
-  else
-    launch_pdl(attn_tc::attn_tc_kernel<64, STREAMS, DIRECT, AHEAD, false, CACHE>, grid, threads, attn_tc::Smem<64, STREAMS>::TOTAL, c->stream, *m.q, *m.k, *m.v, *m.kloc, *m.vloc, a, l.tl);
+  if (c->cfg.head_dim == 128) launch_attention_instance<128, STREAMS, DIRECT, AHEAD, false, CACHE>(c, grid, 1, m, a, l.tl);
+  else launch_attention_instance<64, STREAMS, DIRECT, AHEAD, false, CACHE>(c, grid, 1, m, a, l.tl);
 }
 
 template <bool DIRECT, int CACHE = attn_tc::PLAIN>
@@ -747,7 +745,7 @@ int launch_cache_attention(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
     plan.sink_pages = sink_pages;
     note_route(c, plan);
     Launch l(c, TIDAR_TC_EMBED);
-    launch_pdl(attn_window_plan_kernel, 1, 512, 0, c->stream, w, plan);
+    launch_pdl(attn_window_plan_kernel<CACHE == attn_tc::KV4>, 1, 512, 0, c->stream, w, plan);
   }
   CUtensorMap tq, tk, tv, tkl, tvl;
   bool ok = encode_q_map(c, &tq, x.q, R, x.q_stride);
@@ -941,9 +939,9 @@ template <int HD, int CACHE>
 cudaError_t cache_attention_smem() {
   using namespace attn_tc;
   auto smem = [](const void *f, int bytes) { return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-  cudaError_t e = smem((const void *)attn_tc_kernel<HD, 2, false, false, false, CACHE>, Smem<HD, 2>::TOTAL);
-  if (e == cudaSuccess) e = smem((const void *)attn_tc_kernel<HD, 2, true, false, false, CACHE>, Smem<HD, 2>::TOTAL);
-  if (e == cudaSuccess) e = smem((const void *)attn_tc_kernel<HD, 2, true, false, true, CACHE>, Smem<HD, 2, true>::TOTAL);
+  cudaError_t e = smem((const void *)attn_tc_kernel<HD, 2, false, false, false, CACHE>, Smem<HD, 2, false, CACHE == KV4>::TOTAL);
+  if (e == cudaSuccess) e = smem((const void *)attn_tc_kernel<HD, 2, true, false, false, CACHE>, Smem<HD, 2, false, CACHE == KV4>::TOTAL);
+  if (e == cudaSuccess) e = smem((const void *)attn_tc_kernel<HD, 2, true, false, true, CACHE>, Smem<HD, 2, true, CACHE == KV4>::TOTAL);
   if constexpr (CACHE == WINDOW) {
     const void *f = (const void *)attn_tc_kernel<HD, 1, true, false, false, CACHE>;
     if (e == cudaSuccess) e = smem(f, Smem<HD, 1>::TOTAL);
