@@ -20,8 +20,8 @@ constexpr float LARGEST = 8.507059173023462e37f;      // 2^126: twice that, and 
 
 // Four pairs of values (dimensions 8 w .. 8 w + 7) of word `w`; ss = (s, s), bb = (b, b).
 __device__ __forceinline__ uint32_t pair_of(uint32_t shifted, uint32_t ss, uint32_t bb) {
-  const uint32_t v = (shifted & 0x00780078u) | 0x41804180u;
-  uint32_t r;
+  uint32_t v, r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(v) : "r"(shifted), "r"(0x00780078u), "r"(0x41804180u));      // (shifted & mask) | 16: written in C it became two instructions
   asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(ss), "r"(bb));
   return r;
 }

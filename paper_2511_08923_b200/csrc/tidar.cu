@@ -724,7 +724,12 @@ void launch_attention(tidar_ctx *c, const bf16 *Q, const bf16 *Kp, const bf16 *V
 }
 
 // 4-bit pages: sequences of so few rows per KV head go through attn_few_kernel.
-bool few_rows(const tidar_ctx *c, const WindowRows &w) { return w.rows() * (c->cfg.n_q_heads / c->cfg.n_kv_heads) <= 2 * attn_few::ROWS; }
+bool few_rows(const tidar_ctx *c, const WindowRows &w) { return w.rows() * (c->cfg.n_q_heads / c->cfg.n_kv_heads) <= 2 * attn_few::MAX_ROWS; }
+
+template <int HD, int N8>
+void launch_few_instance(tidar_ctx *c, const attn_few::Args &a) {
+  launch_pdl(attn_few::attn_few_kernel<HD, N8>, a.ctas, attn_few::WARPS * 32, attn_few::Smem<HD, N8>::TOTAL, c->stream, a);
+}
 
 // Calls over a caller's pages on the tensor cores: as tidar_attention's (see attention_direct), except that a tile's pages are those of its window, and that
 // 4-bit pages have no instance of one stream (its warps and the four that turn codes into tiles would not fit an SM twice).
@@ -779,14 +784,15 @@ void launch_few(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
   Launch l(c, TIDAR_TC_ATTN);
   attn_few::Args a{};
   a.c = x; a.n_seqs = n_seqs;
-  a.tiles = (x.rows.rows() * (x.Hq / x.Hkv) + attn_few::ROWS - 1) / attn_few::ROWS;
-  a.ctas = attn_few::CTAS_PER_SM * c->n_sms; a.per_warp = 1;
+  const int rows = x.rows.rows() * (x.Hq / x.Hkv), n8 = rows <= 8 ? 1 : 2;
+  a.tiles = (rows + 8 * n8 - 1) / (8 * n8);
+  a.ctas = attn_few::ctas_per_sm(n8) * c->n_sms; a.per_warp = 1;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)c->cfg.head_dim);
   a.part_O = c->attn_part_O; a.part_ml = c->attn_part_ml; a.arrived = c->d_map + tidar_ctx::FEW_ARRIVED;
-  static_assert(attn_few::CTAS_PER_SM * MAX_SMS * 2 * attn_few::ROWS <= attn_tc::SLOTS_PER_SM * MAX_SMS * 2 * 128 &&
-                tidar_ctx::FEW_ARRIVED + attn_few::CTAS_PER_SM * MAX_SMS <= tidar_ctx::MAP_INTS, "partial results and counters fit the scratch");
-  if (c->cfg.head_dim == 128) launch_pdl(attn_few::attn_few_kernel<128>, a.ctas, attn_few::WARPS * 32, attn_few::Smem<128>::TOTAL, c->stream, a);
-  else launch_pdl(attn_few::attn_few_kernel<64>, a.ctas, attn_few::WARPS * 32, attn_few::Smem<64>::TOTAL, c->stream, a);
+  static_assert(attn_few::MAX_CTAS_PER_SM * MAX_SMS * 2 * attn_few::MAX_ROWS <= attn_tc::SLOTS_PER_SM * MAX_SMS * 2 * 128 &&
+                tidar_ctx::FEW_ARRIVED + attn_few::MAX_CTAS_PER_SM * MAX_SMS <= tidar_ctx::MAP_INTS, "partial results and counters fit the scratch");
+  if (c->cfg.head_dim == 128) { if (n8 == 1) launch_few_instance<128, 1>(c, a); else launch_few_instance<128, 2>(c, a); }
+  else { if (n8 == 1) launch_few_instance<64, 1>(c, a); else launch_few_instance<64, 2>(c, a); }
 }
 
 // How the norm of R rows of d floats with S fp32 partial results each is launched.
@@ -988,8 +994,10 @@ int init_tensor_core_path(tidar_ctx *c) {
     CUDA_TRY(c, cudaMemsetAsync(c->Kloc, 0, nloc * cf.n_kv_heads * cf.head_dim * sizeof(bf16), c->stream));
     CUDA_TRY(c, cudaMemsetAsync(c->Vloc, 0, nloc * cf.n_kv_heads * cf.head_dim * sizeof(bf16), c->stream));
     auto smem = [](const void *f, int bytes) { return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-    CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<128>, attn_few::Smem<128>::TOTAL));
-    CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<64>, attn_few::Smem<64>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<128, 1>, attn_few::Smem<128, 1>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<128, 2>, attn_few::Smem<128, 2>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<64, 1>, attn_few::Smem<64, 1>::TOTAL));
+    CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<64, 2>, attn_few::Smem<64, 2>::TOTAL));
     CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 2, false, false, false, 0>, attn_tc::Smem<128, 2>::TOTAL));
     CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 2, false, true, false, 0>, attn_tc::Smem<128, 2>::TOTAL));
     CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<64, 2, false, false, false, 0>, attn_tc::Smem<64, 2>::TOTAL));
