@@ -27,7 +27,10 @@ namespace attn_few {
 
 constexpr int WARPS = 4, CHUNK = 32, MAX_ROWS = 16, MAX_CTAS_PER_SM = 3;
 constexpr float RAISE_THRESHOLD = 8.f;                 // log2 units (as in attn_tc.cuh)
-__host__ __device__ constexpr int ctas_per_sm(int n8) { return n8 == 1 ? 3 : 2; }      // for 8 n8 rows: what the registers allow
+constexpr int AT_ONCE = 12;                            // partial results of a unit read at once
+// CTAs per SM, for 8 n8 rows: what the registers allow.  With 8 rows there are two instances: three CTAs fill an SM's pipes better, two have the registers to
+// overlap more of a chunk's work (24 sequences of up to 16 k positions 75 and 81 us, one of 32 k 27 and 23).
+__host__ __device__ constexpr int ctas_per_sm(int n8, bool many) { return n8 == 1 && many ? 3 : 2; }
 
 template <int HD, int N8>
 struct Smem {
@@ -39,12 +42,11 @@ struct Smem {
   static constexpr int MERGE_OFF = WARPS * RING, MERGE_BYTES = (O_REGS + STATS) * 32 * 4;
   static constexpr int TOTAL = MERGE_OFF + 2 * MERGE_BYTES;
 };
-static_assert(Smem<128, 1>::TOTAL * ctas_per_sm(1) <= 224 * 1024 && Smem<128, 2>::TOTAL * ctas_per_sm(2) <= 224 * 1024, "CTAs of an SM fit its shared memory");
+static_assert(Smem<128, 1>::TOTAL * ctas_per_sm(1, true) <= 224 * 1024 && Smem<128, 2>::TOTAL * ctas_per_sm(2, true) <= 224 * 1024, "CTAs of an SM fit its shared memory");
 
 struct Args {
   CacheArgs c;
-  int n_seqs, tiles, ctas;            // tiles of 8 n8 rows per (sequence, KV head); CTAs that take shares at most
-  int per_warp;                       // chunks a warp has at least where there are enough
+  int n_seqs, tiles, ctas, most;      // tiles of 8 n8 rows per (sequence, KV head); CTAs that take shares at most, and in calls of fewer than 16 chunks per warp
   float scale_log2;
   float *part_O; float2 *part_ml;     // [2 CTAs][MAX_ROWS][HD], [2 CTAs][MAX_ROWS]
   int32_t *arrived;                   // [CTAs], zero between calls: partial results of the split unit that begins in that CTA's share
@@ -85,12 +87,12 @@ __device__ __forceinline__ Chunks chunks_of(const WindowRows &w, int n) {
   return c;
 }
 
-template <int HD, int N8>
-__global__ void __launch_bounds__(WARPS * 32, ctas_per_sm(N8)) attn_few_kernel(const Args a) {
+template <int HD, int N8, bool MANY>
+__global__ void __launch_bounds__(WARPS * 32, ctas_per_sm(N8, MANY)) attn_few_kernel(const Args a) {
   using L = Smem<HD, N8>;
   constexpr int ROWS = 8 * N8, QK = HD / 16, DT = HD / 4, MT = HD / 16, DV = HD / 8;      // steps of K Q^T; dimensions a lane reads of a key of K; output tiles; dimensions it reads of a key of V
   extern __shared__ __align__(128) uint8_t few_smem[];
-  __shared__ long long sum_s[WARPS];
+  __shared__ long long sums[WARPS][4], sum_s[WARPS];
   __shared__ long long found_base;
   __shared__ int found_seq, is_last;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -101,27 +103,45 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm(N8)) attn_few_kernel(c
 
   // ---- this CTA's share [w0, w1) of all chunks ----
   auto length = [&](int s) { return min(__ldg(wr.seq_len + s), wr.n_max); };
-  auto block_sum = [&](long long v) {
+  const int all0 = threadIdx.x < a.n_seqs ? chunks_of(wr, length(threadIdx.x)).all : 0;       // of this thread's sequence among the first ones
+  auto all_of = [&](int s) { return s < WARPS * 32 ? all0 : chunks_of(wr, length(s)).all; };    // (s = this thread's)
+  // Shares.  While the SMs are not full a warp takes about 1 us per chunk, and merging a unit's p parts 0.15 p us (for that many trips to the L2):
+  // chunks / (4 p) + 0.15 p is least for p = sqrt(1.7 chunks) (12/2 heads, 8 k positions: 63 parts 22.3 us, 31: 17.6, 16: 17.2).  Where two CTAs per SM hold
+  // such parts of all units, those are the shares: one that ends a unit and begins another takes twice as long (32 sequences of up to 200 positions: 14.1 us
+  // with shares that do, 9.5 without).  Otherwise shares are even, across units.
+  int parts_most = 0x7fffffff;
+  auto parts = [&](int all) { return all == 0 ? 0 : min(min((all + WARPS - 1) / WARPS, parts_most), max(1, (int)sqrtf(1.7f * (float)all))); };
+  long long chunks = 0, n_parts_all = 0, units = 0;
+  int longest = 0;
+  for (int s = threadIdx.x; s < a.n_seqs; s += WARPS * 32) {
+    const int all = all_of(s);
+    chunks += all; n_parts_all += parts(all); units += all > 0; longest = max(longest, all);
+  }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
-    if (lane == 0) sum_s[warp] = v;
-    __syncthreads();
-    return sum_s[0] + sum_s[1] + sum_s[2] + sum_s[3];
-  };
-  const long long own0 = threadIdx.x < a.n_seqs ? (long long)chunks_of(wr, length(threadIdx.x)).all * per_seq : 0;
-  long long sum = own0;
-  for (int s = threadIdx.x + WARPS * 32; s < a.n_seqs; s += WARPS * 32) sum += (long long)chunks_of(wr, length(s)).all * per_seq;
-  const long long W = block_sum(sum);
-  const int C = (int)min((W + WARPS * a.per_warp - 1) / (WARPS * a.per_warp), (long long)a.ctas);
+  for (int o = 16; o > 0; o >>= 1) {
+    chunks += __shfl_xor_sync(0xffffffffu, chunks, o); n_parts_all += __shfl_xor_sync(0xffffffffu, n_parts_all, o); units += __shfl_xor_sync(0xffffffffu, units, o);
+    longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
+  }
+  if (lane == 0) { sums[warp][0] = chunks; sums[warp][1] = n_parts_all; sums[warp][2] = units; sums[warp][3] = longest; }
+  __syncthreads();
+  const long long W = (sums[0][0] + sums[1][0] + sums[2][0] + sums[3][0]) * per_seq;
+  n_parts_all = (sums[0][1] + sums[1][1] + sums[2][1] + sums[3][1]) * per_seq; units = (sums[0][2] + sums[1][2] + sums[2][2] + sums[3][2]) * per_seq;
+  longest = (int)max(max(sums[0][3], sums[1][3]), max(sums[2][3], sums[3][3]));
+  bool even = n_parts_all > a.most;
+  int C = (int)min((W + WARPS - 1) / WARPS, (long long)(W >= 16ll * WARPS * a.ctas ? a.ctas : a.most));
+  if (even && units <= a.most) {                       // fewer parts of each unit, where the longest one's then take no longer than even shares and 3 us
+    const int p = a.most / (int)max(units, 1ll);
+    if ((float)longest <= (float)W * (float)p / (float)a.most + 12.f * (float)p) { even = false; parts_most = p; n_parts_all = min(units * p, (long long)a.most); }
+  }
+  if (!even) C = (int)n_parts_all;                     // (with fewer parts than that the last ones find nothing)
   if ((int)blockIdx.x >= C) return;
-  const long long w0 = W * blockIdx.x / C;
-  const int share = (int)(W * (blockIdx.x + 1) / C - w0);
-  {                                                    // the sequence that w0 lies in
+  const long long w0 = even ? W * blockIdx.x / C : blockIdx.x;       // the share's first chunk among all; or its number
+  if (threadIdx.x == 0) found_seq = -1;
+  {                                                    // the sequence that it lies in
     long long base = 0;
     for (int s0 = 0; s0 < a.n_seqs; s0 += WARPS * 32) {
-      const int s = s0 + threadIdx.x;
-      const long long work = s0 == 0 ? own0 : s < a.n_seqs ? (long long)chunks_of(wr, length(s)).all * per_seq : 0;
+      const int s = s0 + threadIdx.x, all = s < a.n_seqs ? all_of(s) : 0;
+      const long long work = (long long)(even ? all : parts(all)) * per_seq;
       long long incl = work;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) { const long long x = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += x; }
@@ -135,13 +155,25 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm(N8)) attn_few_kernel(c
       if (base > w0) break;
     }
     __syncthreads();
+    if (found_seq < 0) return;
   }
 
   // A place among the chunks: chunk c of unit `unit` of sequence `seq`.
   struct Place { int seq, unit, c; Chunks ch; };
   Place here;                                          // of the share's unit that is being worked on
   here.seq = found_seq; here.ch = chunks_of(wr, length(here.seq));
-  here.unit = (int)((w0 - found_base) / here.ch.all); here.c = (int)(w0 - found_base - (long long)here.unit * here.ch.all);
+  int share, part0 = 0, n_parts = 1;                   // its chunks; a unit's parts are those of CTAs part0 .. part0 + n_parts - 1
+  if (even) {
+    here.unit = (int)((w0 - found_base) / here.ch.all); here.c = (int)(w0 - found_base - (long long)here.unit * here.ch.all);
+    share = (int)(W * (blockIdx.x + 1) / C - w0);
+  } else {
+    n_parts = parts(here.ch.all);
+    here.unit = (int)(w0 - found_base) / n_parts;
+    part0 = (int)found_base + here.unit * n_parts;
+    const int j = blockIdx.x - part0;
+    here.c = (int)((long long)here.ch.all * j / n_parts);
+    share = (int)((long long)here.ch.all * (j + 1) / n_parts) - here.c;
+  }
   auto advance = [&](Place &p, int by) {               // (there is such a place)
     p.c += by;
     while (p.c >= p.ch.all) {
@@ -450,8 +482,11 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm(N8)) attn_few_kernel(c
     if (warp < 2) take_over(warp);
     if (warp == 1) hand_over(1);
     __syncthreads();
-    const long long u0 = w0 + done - here.c, u1 = u0 + all;        // the unit among all chunks
-    const int first_cta = cut ? (int)(((u0 + 1) * C - 1) / W) : 0, last_cta = cut ? (int)((u1 * C - 1) / W) : 0;      // shares that its first and last chunk lie in
+    int first_cta = part0, last_cta = part0 + n_parts - 1;         // those whose shares the unit's first and last chunk lie in
+    if (even && cut) {
+      const long long u0 = w0 + done - here.c, u1 = u0 + all;
+      first_cta = (int)(((u0 + 1) * C - 1) / W); last_cta = (int)((u1 * C - 1) / W);
+    }
     if (warp == 0) {
       take_over(1);
 #pragma unroll
@@ -494,19 +529,21 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm(N8)) attn_few_kernel(c
         auto part = [&](int x) { return (size_t)(2 * (first_cta + x) + (x == 0)) * MAX_ROWS + r; };
         float M = -INFINITY, den = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int x0 = 0; x0 < pieces; x0 += 4) {      // four at a time, their loads ahead of the first use
-          float2 ml[4]; float4 v[4];
+        for (int x0 = 0; x0 < pieces; x0 += AT_ONCE) {      // their loads ahead of the first use: a trip to the L2 costs as much as all else
+          float2 ml[AT_ONCE]; float4 v[AT_ONCE];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < AT_ONCE; ++e) {
             ml[e] = make_float2(-INFINITY, 0.f); v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (x0 + e < pieces) { ml[e] = __ldcg(a.part_ml + part(x0 + e)); v[e] = __ldcg(reinterpret_cast<const float4 *>(a.part_O + part(x0 + e) * HD + d)); }
           }
-          const float top = fmaxf(fmaxf(M, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x));
+          float top = M;
+#pragma unroll
+          for (int e = 0; e < AT_ONCE; ++e) top = fmaxf(top, ml[e].x);
           const float keep = M == -INFINITY ? 0.f : exp2f(M - top);
           M = top; den *= keep;
           acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < AT_ONCE; ++e) {
             const float w = ml[e].x == -INFINITY ? 0.f : exp2f(ml[e].x - M);
             den += w * ml[e].y;
             acc.x = fmaf(w, v[e].x, acc.x); acc.y = fmaf(w, v[e].y, acc.y); acc.z = fmaf(w, v[e].z, acc.z); acc.w = fmaf(w, v[e].w, acc.w);

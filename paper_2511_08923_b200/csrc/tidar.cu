@@ -726,9 +726,17 @@ void launch_attention(tidar_ctx *c, const bf16 *Q, const bf16 *Kp, const bf16 *V
 // 4-bit pages: sequences of so few rows per KV head go through attn_few_kernel.
 bool few_rows(const tidar_ctx *c, const WindowRows &w) { return w.rows() * (c->cfg.n_q_heads / c->cfg.n_kv_heads) <= 2 * attn_few::MAX_ROWS; }
 
-template <int HD, int N8>
-void launch_few_instance(tidar_ctx *c, const attn_few::Args &a) {
-  launch_pdl(attn_few::attn_few_kernel<HD, N8>, a.ctas, attn_few::WARPS * 32, attn_few::Smem<HD, N8>::TOTAL, c->stream, a);
+template <int HD, int N8, bool MANY>
+void launch_few_instance(tidar_ctx *c, attn_few::Args &a) {
+  a.ctas = attn_few::ctas_per_sm(N8, MANY) * c->n_sms;
+  a.most = 2 * c->n_sms;
+  launch_pdl(attn_few::attn_few_kernel<HD, N8, MANY>, a.ctas, attn_few::WARPS * 32, attn_few::Smem<HD, N8>::TOTAL, c->stream, a);
+}
+template <int HD>
+void launch_few_rows(tidar_ctx *c, attn_few::Args &a, int n8, bool many) {
+  if (n8 > 1) launch_few_instance<HD, 2, false>(c, a);
+  else if (many) launch_few_instance<HD, 1, true>(c, a);
+  else launch_few_instance<HD, 1, false>(c, a);
 }
 
 // Calls over a caller's pages on the tensor cores: as tidar_attention's (see attention_direct), except that a tile's pages are those of its window, and that
@@ -786,13 +794,14 @@ void launch_few(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
   a.c = x; a.n_seqs = n_seqs;
   const int rows = x.rows.rows() * (x.Hq / x.Hkv), n8 = rows <= 8 ? 1 : 2;
   a.tiles = (rows + 8 * n8 - 1) / (8 * n8);
-  a.ctas = attn_few::ctas_per_sm(n8) * c->n_sms; a.per_warp = 1;
+  // (the lengths are on the device: chunks that the tables have room for, or that the window spans)
+  const long long room = (long long)x.width * 2, span = x.rows.window > 0 ? ((long long)x.rows.window + x.rows.sinks + 2 * x.rows.k) / attn_few::CHUNK + 3 : room;
+  const bool many = std::min(room, span) * n_seqs * x.Hkv * a.tiles >= 16ll * attn_few::WARPS * 3 * c->n_sms;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)c->cfg.head_dim);
   a.part_O = c->attn_part_O; a.part_ml = c->attn_part_ml; a.arrived = c->d_map + tidar_ctx::FEW_ARRIVED;
   static_assert(attn_few::MAX_CTAS_PER_SM * MAX_SMS * 2 * attn_few::MAX_ROWS <= attn_tc::SLOTS_PER_SM * MAX_SMS * 2 * 128 &&
                 tidar_ctx::FEW_ARRIVED + attn_few::MAX_CTAS_PER_SM * MAX_SMS <= tidar_ctx::MAP_INTS, "partial results and counters fit the scratch");
-  if (c->cfg.head_dim == 128) { if (n8 == 1) launch_few_instance<128, 1>(c, a); else launch_few_instance<128, 2>(c, a); }
-  else { if (n8 == 1) launch_few_instance<64, 1>(c, a); else launch_few_instance<64, 2>(c, a); }
+  if (c->cfg.head_dim == 128) launch_few_rows<128>(c, a, n8, many); else launch_few_rows<64>(c, a, n8, many);
 }
 
 // How the norm of R rows of d floats with S fp32 partial results each is launched.
@@ -941,6 +950,15 @@ int forward_rows(tidar_ctx *c, int R, bool with_head, int rows_per_group, const 
 }
 
 // Shared memory that the attention kernels over a caller's pages may claim.
+template <int HD>
+cudaError_t few_attention_smem() {
+  using namespace attn_few;
+  auto smem = [](const void *f, int bytes) { return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
+  cudaError_t e = smem((const void *)attn_few_kernel<HD, 1, true>, Smem<HD, 1>::TOTAL);
+  if (e == cudaSuccess) e = smem((const void *)attn_few_kernel<HD, 1, false>, Smem<HD, 1>::TOTAL);
+  if (e == cudaSuccess) e = smem((const void *)attn_few_kernel<HD, 2, false>, Smem<HD, 2>::TOTAL);
+  return e;
+}
 template <int HD, int CACHE>
 cudaError_t cache_attention_smem() {
   using namespace attn_tc;
@@ -994,10 +1012,8 @@ int init_tensor_core_path(tidar_ctx *c) {
     CUDA_TRY(c, cudaMemsetAsync(c->Kloc, 0, nloc * cf.n_kv_heads * cf.head_dim * sizeof(bf16), c->stream));
     CUDA_TRY(c, cudaMemsetAsync(c->Vloc, 0, nloc * cf.n_kv_heads * cf.head_dim * sizeof(bf16), c->stream));
     auto smem = [](const void *f, int bytes) { return cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-    CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<128, 1>, attn_few::Smem<128, 1>::TOTAL));
-    CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<128, 2>, attn_few::Smem<128, 2>::TOTAL));
-    CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<64, 1>, attn_few::Smem<64, 1>::TOTAL));
-    CUDA_TRY(c, smem((const void *)attn_few::attn_few_kernel<64, 2>, attn_few::Smem<64, 2>::TOTAL));
+    CUDA_TRY(c, few_attention_smem<128>());
+    CUDA_TRY(c, few_attention_smem<64>());
     CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 2, false, false, false, 0>, attn_tc::Smem<128, 2>::TOTAL));
     CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<128, 2, false, true, false, 0>, attn_tc::Smem<128, 2>::TOTAL));
     CUDA_TRY(c, smem((const void *)attn_tc::attn_tc_kernel<64, 2, false, false, false, 0>, attn_tc::Smem<64, 2>::TOTAL));
