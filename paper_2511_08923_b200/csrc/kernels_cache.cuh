@@ -32,75 +32,129 @@ __device__ __forceinline__ uint32_t low_twice(uint32_t sb) { return __byte_perm(
 __device__ __forceinline__ uint32_t high_twice(uint32_t sb) { return __byte_perm(sb, 0, 0x3232); }
 }  // namespace kv4
 
-// Rows of K and V to the slots (64 page + place) that the page map gave them; a slot outside the pool is skipped.  Four threads share a group of 32
-// dimensions, eight each; a thread takes the same place of K and V, so that two loads are on their way at once.  What bounds it: memory, 2.5 bytes an element.
-__global__ void __launch_bounds__(256) kv4_store_kernel(const bf16 *__restrict__ k, long long k_stride, const bf16 *__restrict__ v, long long v_stride, const int32_t *__restrict__ slots,
-                                                        int n_rows, int heads, int hd, uint8_t *__restrict__ k_pages, uint8_t *__restrict__ v_pages, int n_pages) {
-  const int per_head = hd / 8, per_row = heads * per_head;              // threads (a multiple of eight: the four of a group lie in one warp)
-  const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  const long long row = i / per_row;
-  const int at = (int)(i - row * per_row), head = at / per_head, part = at % per_head;
-  const int slot = row < n_rows ? slots[row] : -1;
-  const bool live = slot >= 0 && slot / kv4::PAGE < n_pages;
-  uint4 raw[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-  if (live) {
-    raw[0] = *reinterpret_cast<const uint4 *>(k + row * k_stride + at * 8);
-    raw[1] = *reinterpret_cast<const uint4 *>(v + row * v_stride + at * 8);
+// Blocks of kv4_store_kernel / kv4_load_kernel: threads take eight dimensions each, x along a row (several turns where it has more than KV4_THREADS), y rows.
+constexpr int KV4_THREADS = 256;
+__host__ inline dim3 kv4_block(int heads, int hd) {
+  const int per_row = heads * hd / 8;
+  return per_row < KV4_THREADS ? dim3(per_row, KV4_THREADS / per_row) : dim3(KV4_THREADS, 1);
+}
+
+namespace kv4 {
+// The codes of eight elements as a word.  The quotient is corrected once by its exact remainder, which makes it the correctly rounded one (Markstein: the
+// reciprocal is correctly rounded and s, a bf16 number, not the largest of its binade), so that ties, of which numbers of eight bits have many, are ties.
+__device__ __forceinline__ uint32_t codes8(const float (&x)[8], float s, float b) {
+  constexpr float MAGIC = 12582912.f;                  // 1.5 * 2^23: adding it rounds to an integer, ties to even, which are then the low bits
+  const float inv = __frcp_rn(s);
+  float r[8];                                          // the quotients, rounded, + MAGIC
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float y = x[e] - b, q = y * inv;
+    r[e] = fmaf(fmaf(-q, s, y), inv, q) + MAGIC;
   }
+  if (!(s > 1e-30f && s < 1e30f)) {                    // where remainders or the reciprocal leave the range of normal numbers; and a scale of 0, which gives code 0
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    float x[8];
-    const __nv_bfloat162 *p = reinterpret_cast<const __nv_bfloat162 *>(&raw[which]);
+    for (int e = 0; e < 8; ++e) r[e] = (s > 0.f ? fminf(fmaxf(__fdiv_rn(x[e] - b, s), 0.f), 100.f) : 0.f) + MAGIC;
+  }
+  uint32_t w = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { const float2 f = __bfloat1622float2(p[e]); x[2 * e] = f.x; x[2 * e + 1] = f.y; }
-    float lo = 3e38f, hi = -3e38f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[e] = x[e] != x[e] ? 0.f : fminf(fmaxf(x[e], -kv4::LARGEST), kv4::LARGEST);         // what is held is finite
-      lo = fminf(lo, x[e]); hi = fmaxf(hi, x[e]);
+  for (int e = 0; e < 8; ++e) {
+    const int c = min(max(__float_as_int(r[e]), 0x4b400010), 0x4b40001f) & 15;      // (16 .. 31, less 16)
+    w |= (uint32_t)c << (4 * (e / 2) + 16 * (e % 2));
+  }
+  return w;
+}
+}  // namespace kv4
+
+// Rows of K and V to the slots (64 page + place) that the page map gave them; a slot outside the pool is skipped.  Four threads share a group of 32
+// dimensions, eight each; a thread takes the same place of K and V, so that two loads are on their way at once.  What bounds it: memory, 2.6 bytes an element;
+// most instructions go into the codes.
+template <int HD>
+__global__ void __launch_bounds__(KV4_THREADS) kv4_store_kernel(const bf16 *__restrict__ k, long long k_stride, const bf16 *__restrict__ v, long long v_stride, const int32_t *__restrict__ slots,
+                                                                int n_rows, int heads, uint8_t *__restrict__ k_pages, uint8_t *__restrict__ v_pages, int n_pages) {
+  constexpr int PER_HEAD = HD / 8;
+  const int per_row = heads * PER_HEAD;                // (a multiple of eight: the four threads of a group lie in one warp, full or not)
+  const long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+  const bool there = row < n_rows;
+  pdl_trigger();
+  pdl_wait();
+  const int slot = there ? slots[row] : -1;
+  const bool live = slot >= 0 && slot / kv4::PAGE < n_pages;
+  const int place = slot & (kv4::PAGE - 1);
+  const int first_lane = (threadIdx.y * blockDim.x + threadIdx.x) & ~31, lanes = blockDim.x * blockDim.y - first_lane;
+  const unsigned warp_lanes = lanes >= 32 ? 0xffffffffu : (1u << lanes) - 1;      // (the block's last warp may have fewer)
+  for (int at0 = 0; at0 < per_row; at0 += blockDim.x) {      // (all threads take every turn: the exchange below is of whole warps)
+    const bool has = there && at0 + (int)threadIdx.x < per_row;
+    const int at = has ? at0 + threadIdx.x : 0, head = at / PER_HEAD, part = at % PER_HEAD;
+    uint4 raw[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    if (has) {
+      raw[0] = *reinterpret_cast<const uint4 *>(k + row * k_stride + at * 8);
+      raw[1] = *reinterpret_cast<const uint4 *>(v + row * v_stride + at * 8);
     }
 #pragma unroll
-    for (int o = 1; o < 4; o <<= 1) { lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o)); hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o)); }
-    const bf16 s16 = __float2bfloat16_rn(__fdiv_rn(hi - lo, 15.f));
-    const float s = __bfloat162float(s16);
-    const bf16 b16 = __float2bfloat16_rn(lo - 16.f * s);
-    const float b = __bfloat162float(b16);
-    uint32_t w = 0;
+    for (int which = 0; which < 2; ++which) {
+      uint32_t w[4] = {raw[which].x, raw[which].y, raw[which].z, raw[which].w};
+      // what is held is finite: magnitudes above 2^126 (0x7e80) become that, NaN becomes 0
+      uint32_t large = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float c = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(x[e] - b, s)) - 16.f, 0.f), 15.f) : 0.f;
-      w |= (uint32_t)c << (4 * (e / 2) + 16 * (e % 2));
-    }
-    if (live) {
-      uint8_t *rec = (which ? v_pages : k_pages) + ((size_t)(slot / kv4::PAGE) * heads + head) * kv4::record_bytes(hd);
-      const int place = slot % kv4::PAGE;
-      *reinterpret_cast<uint32_t *>(rec + kv4::word_at(place, part)) = w;
-      if (part % 4 == 0)
-        *reinterpret_cast<uint32_t *>(rec + kv4::code_bytes(hd) + (place * (hd / kv4::GROUP) + part / 4) * 4) =
-            (uint32_t)__bfloat16_as_ushort(s16) | (uint32_t)__bfloat16_as_ushort(b16) << 16;
+      for (int e = 0; e < 4; ++e) large |= (w[e] & 0x7fff7fffu) + 0x017f017fu;
+      if (large & 0x80008000u) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 f = __bfloat1622float2(*reinterpret_cast<__nv_bfloat162 *>(&w[e]));
+          const __nv_bfloat162 h = __floats2bfloat162_rn(f.x != f.x ? 0.f : fminf(fmaxf(f.x, -kv4::LARGEST), kv4::LARGEST), f.y != f.y ? 0.f : fminf(fmaxf(f.y, -kv4::LARGEST), kv4::LARGEST));
+          w[e] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+      }
+      __nv_bfloat162 lo2 = *reinterpret_cast<__nv_bfloat162 *>(&w[0]), hi2 = lo2;
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const __nv_bfloat162 h = *reinterpret_cast<__nv_bfloat162 *>(&w[e]);
+        lo2 = __hmin2(lo2, h); hi2 = __hmax2(hi2, h);
+        const float2 f = __bfloat1622float2(h);
+        x[2 * e] = f.x; x[2 * e + 1] = f.y;
+      }
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) { lo2 = __hmin2(lo2, __shfl_xor_sync(warp_lanes, lo2, o)); hi2 = __hmax2(hi2, __shfl_xor_sync(warp_lanes, hi2, o)); }
+      const float lo = fminf(__low2float(lo2), __high2float(lo2)), hi = fmaxf(__low2float(hi2), __high2float(hi2));
+      const bf16 s16 = __float2bfloat16_rn(__fdiv_rn(hi - lo, 15.f));
+      const float s = __bfloat162float(s16);
+      const bf16 b16 = __float2bfloat16_rn(lo - 16.f * s);
+      const uint32_t code = kv4::codes8(x, s, __bfloat162float(b16));
+      if (has && live) {
+        uint8_t *rec = (which ? v_pages : k_pages) + ((size_t)(slot / kv4::PAGE) * heads + head) * kv4::record_bytes(HD);
+        *reinterpret_cast<uint32_t *>(rec + kv4::word_at(place, part)) = code;
+        if (part % 4 == 0)
+          *reinterpret_cast<uint32_t *>(rec + kv4::code_bytes(HD) + (place * (HD / kv4::GROUP) + part / 4) * 4) = (uint32_t)__bfloat16_as_ushort(s16) | (uint32_t)__bfloat16_as_ushort(b16) << 16;
+      }
     }
   }
 }
 
-// The values at the listed slots as rows of K and V; a row whose slot is outside the pool is left as it is.
-__global__ void __launch_bounds__(256) kv4_load_kernel(const uint8_t *__restrict__ k_pages, const uint8_t *__restrict__ v_pages, int n_pages, const int32_t *__restrict__ slots, int n_rows,
-                                                       int heads, int hd, bf16 *__restrict__ k, long long k_stride, bf16 *__restrict__ v, long long v_stride) {
-  const int per_head = hd / 8, per_row = heads * per_head;
-  const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  const long long row = i / per_row;
+// The values at the listed slots as rows of K and V; a row whose slot is outside the pool is left as it is.  Bound by memory.
+template <int HD>
+__global__ void __launch_bounds__(KV4_THREADS) kv4_load_kernel(const uint8_t *__restrict__ k_pages, const uint8_t *__restrict__ v_pages, int n_pages, const int32_t *__restrict__ slots, int n_rows,
+                                                               int heads, bf16 *__restrict__ k, long long k_stride, bf16 *__restrict__ v, long long v_stride) {
+  constexpr int PER_HEAD = HD / 8;
+  const long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+  pdl_trigger();
+  pdl_wait();
   if (row >= n_rows) return;
-  const int at = (int)(i - row * per_row), head = at / per_head, part = at % per_head;
   const int slot = slots[row];
   if (slot < 0 || slot / kv4::PAGE >= n_pages) return;
-  const size_t rec = ((size_t)(slot / kv4::PAGE) * heads + head) * kv4::record_bytes(hd);
-  const size_t code = rec + kv4::word_at(slot % kv4::PAGE, part), pair = rec + kv4::code_bytes(hd) + (slot % kv4::PAGE * (hd / kv4::GROUP) + part / 4) * 4;
-  const uint32_t wk = *reinterpret_cast<const uint32_t *>(k_pages + code), wv = *reinterpret_cast<const uint32_t *>(v_pages + code);
-  const uint32_t pk = *reinterpret_cast<const uint32_t *>(k_pages + pair), pv = *reinterpret_cast<const uint32_t *>(v_pages + pair);
-  uint32_t o[4];
-  kv4::values8(wk, kv4::low_twice(pk), kv4::high_twice(pk), o);
-  *reinterpret_cast<uint4 *>(k + row * k_stride + at * 8) = make_uint4(o[0], o[1], o[2], o[3]);
-  kv4::values8(wv, kv4::low_twice(pv), kv4::high_twice(pv), o);
-  *reinterpret_cast<uint4 *>(v + row * v_stride + at * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+  const int place = slot & (kv4::PAGE - 1);
+  for (int at = threadIdx.x; at < heads * PER_HEAD; at += blockDim.x) {
+    const int head = at / PER_HEAD, part = at % PER_HEAD;
+    const size_t rec = ((size_t)(slot / kv4::PAGE) * heads + head) * kv4::record_bytes(HD);
+    const size_t code = rec + kv4::word_at(place, part), pair = rec + kv4::code_bytes(HD) + (place * (HD / kv4::GROUP) + part / 4) * 4;
+    const uint32_t wk = *reinterpret_cast<const uint32_t *>(k_pages + code), wv = *reinterpret_cast<const uint32_t *>(v_pages + code);
+    const uint32_t pk = *reinterpret_cast<const uint32_t *>(k_pages + pair), pv = *reinterpret_cast<const uint32_t *>(v_pages + pair);
+    uint32_t o[4];
+    kv4::values8(wk, kv4::low_twice(pk), kv4::high_twice(pk), o);
+    *reinterpret_cast<uint4 *>(k + row * k_stride + at * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+    kv4::values8(wv, kv4::low_twice(pv), kv4::high_twice(pv), o);
+    *reinterpret_cast<uint4 *>(v + row * v_stride + at * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+  }
 }
 
 // ---- page map ------------------------------------------------------------------------------
@@ -123,6 +177,8 @@ __global__ void __launch_bounds__(MAP_THREADS) page_map_kernel(const PageMapArgs
   __shared__ int warp_rows[MAP_THREADS / 32], warp_pages[MAP_THREADS / 32];
   __shared__ int missing, last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_trigger();
+  pdl_wait();
   auto plus = [](int x, int y) { return (int)min((unsigned)x + (unsigned)y, 0x7fffffffu); };
   struct Seq { int n, m, held, want; };
   auto seq_of = [&](int i) {

@@ -804,6 +804,16 @@ void launch_few(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
   if (c->cfg.head_dim == 128) launch_few_rows<128>(c, a, n8, many); else launch_few_rows<64>(c, a, n8, many);
 }
 
+// Launches the instance of the context's head_dim over n_rows rows.
+template <typename K128, typename K64, typename... A>
+void launch_kv4_rows(tidar_ctx *c, K128 kernel_128, K64 kernel_64, int n_rows, A... args) {
+  Launch l(c, TIDAR_TC_ROPE);
+  const dim3 block = kv4_block(c->cfg.n_kv_heads, c->cfg.head_dim);
+  const unsigned grid = (unsigned)(((long long)n_rows + block.y - 1) / block.y);
+  if (c->cfg.head_dim == 128) launch_pdl(kernel_128, grid, block, 0, c->stream, args...);
+  else launch_pdl(kernel_64, grid, block, 0, c->stream, args...);
+}
+
 // How the norm of R rows of d floats with S fp32 partial results each is launched.
 // Behind a projection of many rows the blocks would all crowd onto the SMs that run out of work first (5.6 instead of
 // 3.6 us at 272 rows); claiming a share of the shared memory spreads them evenly.  With few rows they must leave room
@@ -2054,7 +2064,7 @@ int tidar_page_map(tidar_ctx *c, const int32_t *seq_len, const int32_t *n_new, c
   const int grid = std::max((max_rows + MAP_ROWS - 1) / MAP_ROWS, 1);
   {
     Launch l(c, TIDAR_TC_EMBED);
-    page_map_kernel<<<grid, MAP_THREADS, 2 * (n_seqs + 1) * sizeof(int32_t), c->stream>>>(a);
+    launch_pdl(page_map_kernel, grid, MAP_THREADS, 2 * (n_seqs + 1) * sizeof(int32_t), c->stream, a);
   }
   CUDA_TRY(c, cudaGetLastError());
   return TIDAR_OK;
@@ -2067,33 +2077,24 @@ static int check_kv4_rows(tidar_ctx *c, const void *k, int64_t k_stride, const v
   const int row = c->cfg.n_kv_heads * c->cfg.head_dim;
   if (k_stride < row || v_stride < row || k_stride % 8 || v_stride % 8) return fail(c, TIDAR_EINVAL, "row strides must be multiples of 8 elements and hold n_kv_heads * head_dim of them");
   if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)k_pages | (uintptr_t)v_pages) % 16 || (uintptr_t)slots % 4) return fail(c, TIDAR_EINVAL, "tensors must be 16-byte aligned (slots 4-byte)");
-  if ((long long)n_rows * (row / 8) > (long long)INT32_MAX * 256) return fail(c, TIDAR_EINVAL, "too many rows for one call");
   if (!c->inflight.empty()) return fail(c, TIDAR_EINVAL, "a step is in flight");
   return TIDAR_OK;
 }
 
 int tidar_kv4_store(tidar_ctx *c, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *slots, int32_t n_rows, void *k_pages, void *v_pages, int32_t n_pages) {
   if (int rc = check_kv4_rows(c, k, k_stride, v, v_stride, slots, n_rows, k_pages, v_pages, n_pages)) return rc;
-  const tidar_config &cf = c->cfg;
-  const long long threads = (long long)n_rows * cf.n_kv_heads * cf.head_dim / 8;
-  if (threads) {
-    Launch l(c, TIDAR_TC_ROPE);
-    kv4_store_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, c->stream>>>((const bf16 *)k, k_stride, (const bf16 *)v, v_stride, slots, n_rows, cf.n_kv_heads, cf.head_dim,
-                                                                             (uint8_t *)k_pages, (uint8_t *)v_pages, n_pages);
-  }
+  if (n_rows)
+    launch_kv4_rows(c, kv4_store_kernel<128>, kv4_store_kernel<64>, n_rows, (const bf16 *)k, k_stride, (const bf16 *)v, v_stride, slots, n_rows, c->cfg.n_kv_heads, (uint8_t *)k_pages,
+                    (uint8_t *)v_pages, n_pages);
   CUDA_TRY(c, cudaGetLastError());
   return TIDAR_OK;
 }
 
 int tidar_kv4_load(tidar_ctx *c, const void *k_pages, const void *v_pages, int32_t n_pages, const int32_t *slots, int32_t n_rows, void *k, int64_t k_stride, void *v, int64_t v_stride) {
   if (int rc = check_kv4_rows(c, k, k_stride, v, v_stride, slots, n_rows, k_pages, v_pages, n_pages)) return rc;
-  const tidar_config &cf = c->cfg;
-  const long long threads = (long long)n_rows * cf.n_kv_heads * cf.head_dim / 8;
-  if (threads) {
-    Launch l(c, TIDAR_TC_ROPE);
-    kv4_load_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, c->stream>>>((const uint8_t *)k_pages, (const uint8_t *)v_pages, n_pages, slots, n_rows, cf.n_kv_heads, cf.head_dim,
-                                                                            (bf16 *)k, k_stride, (bf16 *)v, v_stride);
-  }
+  if (n_rows)
+    launch_kv4_rows(c, kv4_load_kernel<128>, kv4_load_kernel<64>, n_rows, (const uint8_t *)k_pages, (const uint8_t *)v_pages, n_pages, slots, n_rows, c->cfg.n_kv_heads, (bf16 *)k, k_stride,
+                    (bf16 *)v, v_stride);
   CUDA_TRY(c, cudaGetLastError());
   return TIDAR_OK;
 }
