@@ -712,7 +712,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       else if (CACHE == WINDOW) {                        // (KV4: zeroed where the codes are read)
         const int pos = table_at(l) * PAGE;
         from = n + w.k - pos;
-        if (w.window > 0) { gap0 = max(w.sinks - pos, 0); gap1 = min(n - w.window + 1 - pos, PAGE); }
+        if (w.window > 0) { gap0 = max(w.sinks - pos, 0); gap1 = min(max(n - w.window + 1, 0) - pos, PAGE); }
       }
       return from < PAGE || gap0 < gap1;
     };

@@ -1,5 +1,5 @@
 // A paged cache that the caller keeps: page map of a batch, K and V rows held in 4 bits, and the plain attention over such pages or bf16
-// pages with a sliding window.  (The tensor-core kernels over them: attn_few.cuh, attn_tc.cuh.)
+// pages with a sliding window.  (The kernels that read them fast: attn_few.cuh, attn_tc.cuh.)
 #pragma once
 #include "common.cuh"
 
@@ -299,7 +299,7 @@ struct CacheArgs {
   WindowRows rows;
 };
 
-// One warp per (row, query head), 32 keys at a time, fp32 throughout (impl 1).
+// One warp per (row, query head), 32 keys at a time, fp32 throughout: impl 1.
 template <int HD, bool KV4>
 __global__ void __launch_bounds__(32) attn_cache_replay_kernel(const CacheArgs a, float scale) {
   constexpr int DPL = HD / 32;

@@ -789,6 +789,7 @@ int launch_cache_attention(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
 }
 
 void launch_few(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
+  c->route = {1, false, 0};
   Launch l(c, TIDAR_TC_ATTN);
   attn_few::Args a{};
   a.c = x; a.n_seqs = n_seqs;
@@ -2119,8 +2120,11 @@ static int attention_over_cache(tidar_ctx *c, const tidar_attention_args *x, boo
       ((uintptr_t)x->page_table | (uintptr_t)x->seq_len) % 4)
     return fail(c, TIDAR_EINVAL, "tensors must be 16-byte aligned (page_table and seq_len 4-byte)");
   if (!c->inflight.empty()) return fail(c, TIDAR_EINVAL, "a step is in flight");
+  // a window that reaches back to position 0 from every slot is none, and sinks behind the table's positions are no more than those
+  const long long positions = (long long)x->pages_per_seq * 64;
+  const int window = x->window >= positions + x->k ? 0 : x->window, sinks = (int)std::min<long long>(x->sinks, positions);
   CacheArgs a{(const bf16 *)x->q, q_stride, x->k_pages, x->v_pages, x->n_pages, x->page_table, x->pages_per_seq, (const bf16 *)x->k_local, (const bf16 *)x->v_local, local_stride,
-              (bf16 *)x->out, cf.n_q_heads, cf.n_kv_heads, WindowRows{x->seq_len, x->k, blocks, x->pages_per_seq * 64 - x->k, x->window, x->sinks}};
+              (bf16 *)x->out, cf.n_q_heads, cf.n_kv_heads, WindowRows{x->seq_len, x->k, blocks, x->pages_per_seq * 64 - x->k, window, sinks}};
   if (cf.impl == 0) {
     if (four_bits && few_rows(c, a.rows)) launch_few(c, a, x->n_seqs);
     else if (int rc = four_bits ? launch_cache_attention<attn_tc::KV4>(c, a, x->n_seqs) : launch_cache_attention<attn_tc::WINDOW>(c, a, x->n_seqs)) return rc;

@@ -288,6 +288,48 @@ def test_absent_sequences_and_pages_outside_the_pool(impl, kv4):
     t.close()
 
 
+@pytest.mark.parametrize("impl", IMPLS)
+@pytest.mark.parametrize("kv4", [True, False])
+def test_mostly_local_rows_and_the_largest_windows(impl, kv4):
+    t = H.lib_context(128, 8, 2, 600, impl=impl)
+    _attention_case(t, kv4, 128, 8, 2, 16, True, [0, 64], 0, 0, 46)
+    _attention_case(t, kv4, 128, 8, 2, 16, True, [5], 1, 0, 47)
+    _attention_case(t, kv4, 128, 8, 2, 3, True, [0, 1], 1, 1, 48)
+    big = 2 ** 31 - 1
+    for k, blocks, ns in ((1, False, [700, 0]), (5, True, [300]), (90, False, [70])):
+        _attention_case(t, kv4, 128, 8, 2, k, blocks, ns, big, big, 49)
+        _attention_case(t, kv4, 128, 8, 2, k, blocks, ns, 64, big, 50)
+        _attention_case(t, kv4, 128, 8, 2, k, blocks, ns, big, 0, 51)
+    t.close()
+
+
+@pytest.mark.parametrize("kv4", [True, False])
+@pytest.mark.parametrize("B,k,blocks,n", [(1, 1, False, 20000), (3, 1, False, 5000), (40, 1, False, 900), (1, 4, True, 9000), (1, 16, True, 4000), (2, 2, True, 3000)])
+def test_a_call_gives_the_same_bits_every_time(kv4, B, k, blocks, n):
+    """Partial results are merged in one order, whichever CTA does it; and a call leaves the scratch as it found it."""
+    hd, Hq, Hkv = 128, 8, 2
+    t = H.lib_context(hd, Hq, Hkv, 300)
+    g = torch.Generator(device="cuda:0").manual_seed(4)
+    width = (n + k + 63) // 64
+    if kv4:
+        from paper_2511_08923_b200 import kv4_page_bytes, kv4_pages
+        pools = [kv4_pages(B * width, Hkv, hd) for _ in range(2)]
+        for p in pools:
+            x = torch.randn(B * width * 64, Hkv, hd, device="cuda:0", generator=g).to(torch.bfloat16)
+            t.kv4_store(x, x, torch.arange(B * width * 64, dtype=torch.int32, device="cuda:0"), p, p)
+    else:
+        pools = [torch.randn(B * width, Hkv, 64, hd, device="cuda:0", generator=g).to(torch.bfloat16) for _ in range(2)]
+    T = k * (k + 1) if blocks else k
+    q, kl, vl = (torch.randn(r, h, hd, device="cuda:0", generator=g).to(torch.bfloat16) for r, h in ((B * T, Hq), (B * k * k, Hkv), (B * k * k, Hkv)))
+    table, sl = torch.arange(B * width, dtype=torch.int32, device="cuda:0").view(B, width), _i32([n - 37 * i for i in range(B)])
+    outs = [torch.zeros(B * T, Hq * hd, dtype=torch.bfloat16, device="cuda:0") for _ in range(12)]
+    for o in outs:
+        (t.attention_kv4 if kv4 else t.attention_window)(q, *pools, table, sl, kl if blocks else None, vl if blocks else None, o, B, k, window=0)
+    t.sync()
+    assert all(torch.equal(o, outs[0]) for o in outs) and outs[0].isfinite().all() and outs[0].abs().sum() > 0
+    t.close()
+
+
 @pytest.mark.parametrize("kv4", [True, False])
 def test_lengths_beyond_the_table_are_clamped(kv4):
     t = H.lib_context(64, 4, 2, 64)
