@@ -185,8 +185,8 @@ constexpr int CAND = 32;                               // limits tried per pairi
 // The estimate, for the plan kernel and for the host, which decides with it whether a step's merge kernel is needed at all (step_attention): limit number i
 // of the units or tiles the longest of which takes `longest` us; pieces of an entity of `us` us, at most one per page; what all entities come to.
 struct PlanCost { int items, live, most; float sum, longest; };
-// 4-bit pages (CODES) cost a single tile more: its turn is as long as the warps that fill the tiles take, which in a pair two tiles share.
-constexpr float CODES_PAIR_PAGE = 1.3f, CODES_SINGLE_PAGE = 0.92f;
+// 4-bit pages (CODES) cost more: the warps that fill the tiles and the softmax warps take turns at issuing (measured inside a step of 272 rows, 32 k positions).
+constexpr float CODES_PAIR_PAGE = 1.33f, CODES_SINGLE_PAGE = 0.84f;
 template <bool CODES> __host__ __device__ constexpr float page_us(bool pair) { return CODES ? (pair ? CODES_PAIR_PAGE : CODES_SINGLE_PAGE) : pair ? PAIR_PAGE : SINGLE_PAGE; }
 __host__ __device__ inline float plan_limit(float longest, int i) { return fmaxf(longest / (1.f + 0.5f * i), 0.1f) * 1.0001f; }
 template <bool CODES = false>
@@ -1043,6 +1043,15 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       uint32_t st_l = lane == 2 ? 1u : 0u, par_l = lane == 2 ? 0u : 1u;
       static_assert(L::CODE_STAGES >= 2 || CACHE != KV4, "turn 1's codes are in stage 1");
       int sk = 0, sv = 0, c = 1;                         // the turn's stages (c: of the next one's codes)
+      // A tile is announced a turn late, behind the next turn's wait: by then its stores are done and the fence in front of the announcement costs nothing
+      // (230 -> 221 us at 32 k positions).  That next turn waits for nothing that this one's tiles have to be there for: its K tile takes the place of page i - 3,
+      // whose product, with the V product that frees its V tile, was released by tiles of earlier turns.
+      uint32_t full = 0u;                                // the barrier that this lane has yet to arrive on
+      auto announce = [&] {
+        sm100::fence_proxy_async();
+        __syncwarp();
+        if (full) sm100::mbar_arrive(full);
+      };
       Codes xk{}, xv{};
       bool ok = true;
       if (code_turns > 0) {
@@ -1054,13 +1063,14 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       for (int i = 0; ok && i < np + lead; ++i) {
         const bool mine = i >= from && i < to;
         if (!(ok = sm100::mbar_wait_lanes(mine ? wait0 + st_l * 8u : 0u, par_l, abortp))) break;
+        announce();
         const int vp = i - lead;
         const Codes nk = read(i + 1, 0, c), nv = read(vp + 1, 1, c);
         if (i < n_table) { if (does_k) write(xk, i, L::K_OFF + (uint32_t)sk * L::KV_BYTES); } else if (i < np) load_local(i, 0, sk);
         if (vp >= 0) { if (vp < n_table) { if (does_v) write(xv, vp, L::V_OFF + (uint32_t)sv * L::KV_BYTES); } else load_local(vp, 1, sv); }
-        sm100::fence_proxy_async();
         __syncwarp();
-        if (mine && arrives && i < by_load) sm100::mbar_arrive(done0 + st_l * 8u);
+        full = mine && arrives && i < by_load ? done0 + st_l * 8u : 0u;
+        if (lane == 2) { if (full) sm100::mbar_arrive(full); full = 0u; }      // (codes: read)
         if (mine && (int)++st_l == ring) { st_l = 0; par_l ^= 1u; }
         xk = nk; xv = nv;
         if (++sk == L::K_STAGES) sk = 0;
@@ -1068,6 +1078,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         if (++c == L::CODE_STAGES) c = 0;
         __syncwarp();
       }
+      announce();
     }
   }
   if constexpr (CLUSTER) {
