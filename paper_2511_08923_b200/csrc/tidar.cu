@@ -751,6 +751,10 @@ int launch_cache_attention(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
   const int n_pages = w.window > 0 ? (int)std::min<long long>(x.width, ((long long)w.window + span) / 64 + 2 + sink_pages) : x.width;
   DirectPlan d = attention_direct(c, n_seqs, T, n_pages);
   if (CACHE == attn_tc::KV4 && d.streams == 1) d.streams = 0;
+  // One sequence: its tiles have about the same pages, so the SMs share them evenly without a plan where that comes to two parts of each or more (32/8 heads, 272
+  // rows, a window of 4 k: 37.0 us planned, 33.9 not; 4 bits, 32 k positions 224 and 215); uncut while a plan that cuts pairs would gain no more than it costs.
+  const int tiles = n_seqs * ((T + spt - 1) / spt) * x.Hkv;
+  if (!d.streams && n_seqs == 1 && (2 * tiles <= c->n_sms || (tiles <= c->n_sms && n_pages <= (CACHE == attn_tc::KV4 ? 24 : 45)))) d = {2, std::min<int>(attn_tc::MAX_SPLITS, c->n_sms / tiles), 1};
   attn_tc::PlanArgs plan{};
   if (!d.streams) {
     c->split_keys = may_split((int)std::min<long long>((long long)n_pages * 64, INT32_MAX)); c->attn_cluster = 1;
@@ -774,7 +778,6 @@ int launch_cache_attention(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
   if (d.streams) {
     c->route = {d.cluster, d.pieces > 1, 0};
     a.direct.pieces = d.pieces; a.direct.per_group = (T + spt - 1) / spt;
-    const int tiles = n_seqs * a.direct.per_group * a.Hkv;
     if constexpr (CACHE == attn_tc::WINDOW) {
       if (d.streams == 1) { launch_attention_kernel<1, true, false, CACHE>(c, tiles, am, a); return TIDAR_OK; }
     }
