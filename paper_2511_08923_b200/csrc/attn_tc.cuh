@@ -784,7 +784,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
     auto pool_bits = [&](int j) {
       const int l = p_begin + (shared ? j + lane : 2 * (j + lane) + t);
       const int32_t *table = a.page_table + (size_t)item.seq * a.pages_per_seq;
-      return __ballot_sync(0xffffffffu, l < min(item.n_cache_pages, item.p_end) && (unsigned)__ldg(table + table_at(l)) < (unsigned)a.win.n_pages);
+      return __ballot_sync(0xffffffffu, l < min(item.n_cache_pages, item.p_end) && (unsigned)table[table_at(l)] < (unsigned)a.win.n_pages);
     };
     unsigned in_pool = 0;
     if constexpr (CACHE != PLAIN) in_pool = pool_bits(0);

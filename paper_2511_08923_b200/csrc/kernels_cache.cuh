@@ -69,8 +69,8 @@ __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float s, float b
 // dimensions, eight each; a thread takes the same place of K and V, so that two loads are on their way at once.  What bounds it: memory, 2.6 bytes an element;
 // most instructions go into the codes.
 template <int HD>
-__global__ void __launch_bounds__(KV4_THREADS) kv4_store_kernel(const bf16 *__restrict__ k, long long k_stride, const bf16 *__restrict__ v, long long v_stride, const int32_t *__restrict__ slots,
-                                                                int n_rows, int heads, uint8_t *__restrict__ k_pages, uint8_t *__restrict__ v_pages, int n_pages) {
+__global__ void __launch_bounds__(KV4_THREADS) kv4_store_kernel(const bf16 *k, long long k_stride, const bf16 *v, long long v_stride, const int32_t *slots,
+                                                                int n_rows, int heads, uint8_t *k_pages, uint8_t *v_pages, int n_pages) {
   constexpr int PER_HEAD = HD / 8;
   const int per_row = heads * PER_HEAD;                // (a multiple of eight: the four threads of a group lie in one warp, full or not)
   const long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
@@ -131,10 +131,11 @@ __global__ void __launch_bounds__(KV4_THREADS) kv4_store_kernel(const bf16 *__re
   }
 }
 
+// (No __restrict__: rows, slots and pages may be the previous kernel's output, which ends after this one has begun.)
 // The values at the listed slots as rows of K and V; a row whose slot is outside the pool is left as it is.  Bound by memory.
 template <int HD>
-__global__ void __launch_bounds__(KV4_THREADS) kv4_load_kernel(const uint8_t *__restrict__ k_pages, const uint8_t *__restrict__ v_pages, int n_pages, const int32_t *__restrict__ slots, int n_rows,
-                                                               int heads, bf16 *__restrict__ k, long long k_stride, bf16 *__restrict__ v, long long v_stride) {
+__global__ void __launch_bounds__(KV4_THREADS) kv4_load_kernel(const uint8_t *k_pages, const uint8_t *v_pages, int n_pages, const int32_t *slots, int n_rows,
+                                                               int heads, bf16 *k, long long k_stride, bf16 *v, long long v_stride) {
   constexpr int PER_HEAD = HD / 8;
   const long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   pdl_trigger();

@@ -723,7 +723,8 @@ void launch_attention(tidar_ctx *c, const bf16 *Q, const bf16 *Kp, const bf16 *V
     attn_replay_kernel<64><<<grid, 32, 0, c->stream>>>(Q, Kp, Vp, g, c->meta, Kl, Vl, O, c->cfg.n_q_heads, scale);
 }
 
-// 4-bit pages: sequences of so few rows per KV head go through attn_few_kernel.
+// 4-bit pages: sequences of so few rows per KV head go through attn_few_kernel (24 sequences of up to 9 k positions, 32/8 heads: 16 rows 82 us there and 164 through
+// the 128-row tiles, 32 rows 152 and 164, 48 rows 217 and 165; one of 2 k positions 16.3 / 15.0, 16.9 / 15.0, 17.1 / 15.1).
 bool few_rows(const tidar_ctx *c, const WindowRows &w) { return w.rows() * (c->cfg.n_q_heads / c->cfg.n_kv_heads) <= 2 * attn_few::MAX_ROWS; }
 
 template <int HD, int N8, bool MANY>
