@@ -102,8 +102,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm(N8, MANY)) attn_few_ke
   pdl_wait();
 
   // ---- this CTA's share [w0, w1) of all chunks ----
-  // (tables and lengths may be the previous kernel's output, which ends after this one has begun: they are read from the L2)
-  auto length = [&](int s) { return min(__ldcg(wr.seq_len + s), wr.n_max); };
+  auto length = [&](int s) { return min(wr.seq_len[s], wr.n_max); };
   const int all0 = threadIdx.x < a.n_seqs ? chunks_of(wr, length(threadIdx.x)).all : 0;       // of this thread's sequence among the first ones
   auto all_of = [&](int s) { return s < WARPS * 32 ? all0 : chunks_of(wr, length(s)).all; };    // (s = this thread's)
   // Shares.  While the SMs are not full a warp takes about 1 us per chunk, and merging a unit's p parts 0.15 p us (for that many trips to the L2):
@@ -192,7 +191,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm(N8, MANY)) attn_few_ke
   Place f = here;                                      // of the chunk that is fetched next, number f_at of the share
   int f_at = warp, f_page = -1;                        // its page, read when the chunk before it was fetched
   auto chunk_of = [&](const Place &p) { return p.c < p.ch.sink ? p.c : p.c + p.ch.skip; };
-  auto look_up = [&] { f_page = f_at < share && f.c < f.ch.cached ? __ldcg(a.c.table + (size_t)f.seq * a.c.width + (chunk_of(f) >> 1)) : -1; };
+  auto look_up = [&] { f_page = f_at < share && f.c < f.ch.cached ? a.c.table[(size_t)f.seq * a.c.width + (chunk_of(f) >> 1)] : -1; };
   if (f_at < share) advance(f, warp);
   look_up();
   auto fetch = [&](int stage) {
