@@ -164,6 +164,7 @@ class Tidar:
         self.shape, self.k_max, self.max_batch = shape, k_max, max_batch
         self._async_n = []                   # listed sequences of the steps in flight, oldest first
         self.device = torch.device(device)
+        self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         cfg = tidar_config(
             n_layers=len(packed["layers"]), d_model=shape.d_model, n_q_heads=shape.n_q_heads, n_kv_heads=shape.n_kv_heads,
             head_dim=shape.head_dim, d_ffn=shape.d_ffn, vocab=shape.vocab, tie_lm_head=int(shape.tie_lm_head),
@@ -410,38 +411,52 @@ class Tidar:
             seq_len.data_ptr(), k_local.data_ptr(), v_local.data_ptr(), out.data_ptr(), n_seqs, k))
 
     # -- a paged cache that the caller keeps -----------------------------------
-    def _tensor(self, name, x, dtype, shape, row_strided=False):
-        """Checks a caller's tensor (its device, type, shape, layout) and returns its address."""
-        if isinstance(x, torch.Tensor) and x.dtype is dtype and x.get_device() == self._device_index() and x.shape == shape and x.is_contiguous():
-            return x.data_ptr()
-        if not isinstance(x, torch.Tensor):
-            raise ValueError(f"{name} must be a tensor")
-        if x.get_device() != self._device_index():
-            raise ValueError(f"{name} is on {x.device}, the context on {self.device}")
-        if x.dtype != dtype:
-            raise ValueError(f"{name} must be {dtype}, not {x.dtype}")
-        if x.shape != shape:
-            raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(x.shape)}")
-        if not row_strided or not x[0].is_contiguous() or (x.shape[0] > 1 and x.stride(0) < x[0].numel()):
-            raise ValueError(f"{name} must be contiguous" + (" within a row, its rows apart" if row_strided else ""))
-        return x.data_ptr()
+    def _tensor(self, name, x, dtype, shape):
+        """Checks a caller's tensor (device, type, shape, contiguous) and returns its address.  (A loop makes such calls per layer: the checks are one expression.)"""
+        try:
+            if x.dtype is dtype and x.get_device() == self._index and x.shape == shape and x.is_contiguous():
+                return x.data_ptr()
+        except AttributeError:
+            pass
+        raise self._unfit(name, x, dtype, shape, "contiguous")
 
-    def _device_index(self):
-        return self.device.index if self.device.index is not None else torch.cuda.current_device()
+    def _rows(self, name, x, dtype, shape):
+        """The same for rows [rows, heads, head_dim] that may lie apart: their address and stride."""
+        try:
+            if x.dtype is dtype and x.get_device() == self._index and x.shape == shape:
+                n, h, d = shape
+                s = x.stride()
+                if s[2] == 1 and (s[1] == d or h == 1) and (s[0] >= h * d or n <= 1):
+                    return x.data_ptr(), s[0] if n > 1 else h * d
+        except AttributeError:
+            pass
+        raise self._unfit(name, x, dtype, shape, "contiguous within a row, its rows apart")
+
+    def _unfit(self, name, x, dtype, shape, layout):
+        if not isinstance(x, torch.Tensor):
+            return ValueError(f"{name} must be a tensor")
+        if x.get_device() != self._index:
+            return ValueError(f"{name} is on {x.device}, the context on cuda:{self._index}")
+        if x.dtype != dtype:
+            return ValueError(f"{name} must be {dtype}, not {x.dtype}")
+        if x.shape != shape:
+            return ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(x.shape)}")
+        return ValueError(f"{name} must be {layout}")
 
     def _on_device(self, entry, *args):
         """Calls a library entry with the context's device current."""
-        if torch.cuda.current_device() == self._device_index():
+        if torch.cuda.current_device() == self._index:
             self._check(entry(self.ctx, *args))
         else:
-            with torch.cuda.device(self.device):
+            with torch.cuda.device(self._index):
                 self._check(entry(self.ctx, *args))
 
     @staticmethod
     def _length(name, x, dim=0):
-        if not isinstance(x, torch.Tensor) or x.dim() <= dim:
-            raise ValueError(f"{name} must be a tensor of at least {dim + 1} dimensions")
-        return x.shape[dim]
+        try:
+            return x.shape[dim]
+        except (AttributeError, IndexError):
+            raise ValueError(f"{name} must be a tensor of at least {dim + 1} dimensions") from None
 
     def page_map(self, seq_len, n_new, held, free_pages, page_table, held_out, row_start, slots, counts, free_begin=None):
         """Page table entries and slots for the rows that sequences are about to get (see tidar_page_map).
@@ -459,19 +474,18 @@ class Tidar:
     def _kv4_rows(self, k, v, slots, k_pages, v_pages):
         hkv, hd, rows, n_pages = self.shape.n_kv_heads, self.shape.head_dim, self._length("slots", slots), self._length("k_pages", k_pages)
         shape, pool = (rows, hkv, hd), (n_pages, hkv, kv4_page_bytes(hd))
-        return (self._tensor("k", k, torch.bfloat16, shape, True), self._tensor("v", v, torch.bfloat16, shape, True), self._tensor("slots", slots, torch.int32, (rows,)),
-                self._tensor("k_pages", k_pages, torch.uint8, pool), self._tensor("v_pages", v_pages, torch.uint8, pool), rows, n_pages,
-                k.stride(0) if rows > 1 else hkv * hd, v.stride(0) if rows > 1 else hkv * hd)
+        return (*self._rows("k", k, torch.bfloat16, shape), *self._rows("v", v, torch.bfloat16, shape), self._tensor("slots", slots, torch.int32, (rows,)),
+                self._tensor("k_pages", k_pages, torch.uint8, pool), self._tensor("v_pages", v_pages, torch.uint8, pool), rows, n_pages)
 
     def kv4_store(self, k, v, slots, k_pages, v_pages):
         """Rows of K and V [rows, n_kv_heads, head_dim] (rows may be strided) into 4-bit pages (see tidar_kv4_store)."""
-        pk, pv, ps, kp, vp, rows, n_pages, sk, sv = self._kv4_rows(k, v, slots, k_pages, v_pages)
+        pk, sk, pv, sv, ps, kp, vp, rows, n_pages = self._kv4_rows(k, v, slots, k_pages, v_pages)
         if rows:
             self._on_device(self.lib.tidar_kv4_store, pk, sk, pv, sv, ps, rows, kp, vp, n_pages)
 
     def kv4_load(self, k_pages, v_pages, slots, k, v):
         """The values that slots of 4-bit pages stand for, into rows of K and V (see tidar_kv4_load)."""
-        pk, pv, ps, kp, vp, rows, n_pages, sk, sv = self._kv4_rows(k, v, slots, k_pages, v_pages)
+        pk, sk, pv, sv, ps, kp, vp, rows, n_pages = self._kv4_rows(k, v, slots, k_pages, v_pages)
         if rows:
             self._on_device(self.lib.tidar_kv4_load, kp, vp, n_pages, ps, rows, pk, sk, pv, sv)
 
@@ -484,11 +498,11 @@ class Tidar:
         local_stride = 0
         if blocks:
             shape = (n_seqs * k * k, hkv, hd)
-            pkl, pvl = tensor("k_local", k_local, bf16, shape, True), tensor("v_local", v_local, bf16, shape, True)
-            local_stride = k_local.stride(0) if shape[0] > 1 else 0
-            if shape[0] > 1 and v_local.stride(0) != local_stride:
+            (pkl, local_stride), (pvl, stride) = self._rows("k_local", k_local, bf16, shape), self._rows("v_local", v_local, bf16, shape)
+            if stride != local_stride:
                 raise ValueError("k_local and v_local must have the same row stride")
-        args = tidar_attention_args(tensor("q", q, bf16, (rows, hq, hd), True), q.stride(0) if rows > 1 else 0, tensor("k_pages", k_pages, dtype, pool), tensor("v_pages", v_pages, dtype, pool),
+        pq, q_stride = self._rows("q", q, bf16, (rows, hq, hd))
+        args = tidar_attention_args(pq, q_stride, tensor("k_pages", k_pages, dtype, pool), tensor("v_pages", v_pages, dtype, pool),
                                     n_pages, tensor("page_table", page_table, torch.int32, (n_seqs, width)), width, tensor("seq_len", seq_len, torch.int32, (n_seqs,)), pkl, pvl,
                                     local_stride, tensor("out", out, bf16, (rows, hq * hd)), n_seqs, k, window, sinks)
         self._on_device(entry, C.byref(args))

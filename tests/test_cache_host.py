@@ -27,10 +27,26 @@ def test_calls_without_a_context_are_refused():
 
 def test_the_binding_refuses_tensors_of_another_device_type_or_shape():
     t = Tidar.__new__(Tidar)
-    t.device = torch.device("cuda:0")
+    t._index = 0
     for x in (torch.zeros(3), torch.zeros(3, dtype=torch.int32), None, [1, 2]):
         with pytest.raises(ValueError):
             t._tensor("x", x, torch.float32, (3,))
+    t._index = -1                                        # (where a CPU tensor says it is, so that the other checks are reached)
+    x = torch.zeros(4, 6, 8)
+    assert t._tensor("x", x, torch.float32, (4, 6, 8)) == x.data_ptr()
+    assert t._rows("x", x[:, 1:3], torch.float32, (4, 2, 8)) == (x.data_ptr() + 32, 48)
+    assert t._rows("x", x[:1, 1:3], torch.float32, (1, 2, 8)) == (x.data_ptr() + 32, 16) and t._rows("x", x[:, 2:3], torch.float32, (4, 1, 8))[1] == 48
+    assert t._rows("x", x[:0], torch.float32, (0, 6, 8))[1] == 48
+    for bad, dtype, shape in ((x[:, :, ::2], torch.float32, (4, 6, 4)), (x[:, ::2], torch.float32, (4, 3, 8)), (x.transpose(0, 1), torch.float32, (6, 4, 8)), (x.half(), torch.float32, (4, 6, 8)),
+                              (x, torch.float32, (4, 6, 9)), (x[:1].expand(4, 6, 8), torch.float32, (4, 6, 8)), (x[0], torch.float32, (4, 6, 8)), (None, torch.float32, (1, 1, 1))):
+        with pytest.raises(ValueError):
+            t._rows("x", bad, dtype, shape)
+    with pytest.raises(ValueError):
+        t._tensor("x", x[:, 1:3], torch.float32, (4, 2, 8))
+    with pytest.raises(ValueError):
+        Tidar._length("x", torch.zeros(3), 1)
+    with pytest.raises(ValueError):
+        Tidar._length("x", [1], 0)
 
 
 def test_argument_struct_is_laid_out_as_in_c(tmp_path):
