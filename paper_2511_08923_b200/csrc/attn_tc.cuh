@@ -486,7 +486,7 @@ __device__ __noinline__ void finish_alone(uint32_t o_addr, int t, int my_row, fl
 // zero times a V that is not a number would, so such rows of V are zeroed: by the watcher, in the few pages that have any (WINDOW, and local rows), before it
 // releases their product.
 //   KV4: the load warps bring records of codes, and eight more warps turn them into bf16 tiles in the layout that a TMA load would have given.  A page's
-//   16 K elements of K and V cost them 130 instructions each.
+//   16 K elements of K and V cost each of them 100 instructions, and the turn another 170.
 template <int HD, int STREAMS, bool DIRECT, bool AHEAD, bool CLUSTER, int CACHE>
 __global__ void __launch_bounds__(threads(STREAMS, CACHE), 3 - STREAMS)
 attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,

@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(MAP_THREADS) page_map_kernel(const PageMapArgs
   __syncthreads();
   if (!last) return;
   // every CTA has read what may be overwritten in place
-  for (int i = tid; i < a.n_seqs; i += MAP_THREADS) { const Seq s = seq_of(i); a.held_out[i] = max(s.held, s.want); }
+  for (int i = tid; i < a.n_seqs; i += MAP_THREADS) a.held_out[i] = max(a.held[i], seq_of(i).want);
   if (tid == 0) {
     __threadfence();
     const int without = *reinterpret_cast<volatile int32_t *>(&a.scratch[1]);

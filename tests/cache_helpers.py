@@ -53,7 +53,7 @@ def page_map(n, m, held, free, begin, table, max_rows):
     for i in range(len(n)):
         rows = max(int(m[i]), 0) if n[i] >= 0 else 0
         want = min((int(n[i]) + rows + PAGE - 1) // PAGE, width) if n[i] >= 0 else 0
-        for e in range(held[i], want):
+        for e in range(max(held[i], 0), want):
             table[i, e] = free[at] if at < len(free) else -1
             at += 1
         held[i] = max(held[i], want)

@@ -66,6 +66,7 @@ def test_page_map_when_the_table_or_the_list_ends():
     _map_case(t, n, m, held, free, 0, table, 260)
     _map_case(t, n, m, held, free[:1], 0, table, 260)            # one page for three
     _map_case(t, n, m, held, free[:0], 0, table, 260)
+    _map_case(t, np.array([100, -1, 70, -9]), np.array([60, 5, 200, 5]), np.array([-3, -4, 9, 9]), free, 0, table, 260, True)       # counts of held pages that make no sense
     _map_case(t, np.array([2 ** 31 - 1]), np.array([300]), np.array([4]), free, 0, table[:1], 70)          # positions beyond 32 bits
     t.close()
 
@@ -190,7 +191,7 @@ def _attention_case(t, kv4, hd, Hq, Hkv, k, blocks, ns, window, sinks, seed, fus
     return got
 
 
-HEADS = [(64, 4, 2), (128, 8, 2), (128, 12, 2), (128, 4, 4), (128, 7, 1)]
+HEADS = [(64, 4, 2), (128, 8, 2), (128, 12, 2), (128, 4, 4), (128, 7, 1), (64, 20, 1)]
 IMPLS = [1, 0]
 
 
