@@ -40,6 +40,12 @@ __host__ inline dim3 kv4_block(int heads, int hd) {
 }
 
 namespace kv4 {
+// d / 15, correctly rounded in the same way (see below).
+__device__ __forceinline__ float fifteenth(float d) {
+  constexpr float R = 1.f / 15.f;
+  const float q = d * R;
+  return d > 1e-30f ? fmaf(fmaf(-q, 15.f, d), R, q) : __fdiv_rn(d, 15.f);
+}
 // The codes of eight elements as a word.  The quotient is corrected once by its exact remainder, which makes it the correctly rounded one (Markstein: the
 // reciprocal is correctly rounded and s, a bf16 number, not the largest of its binade), so that ties, of which numbers of eight bits have many, are ties.
 __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float s, float b) {
@@ -55,13 +61,15 @@ __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float s, float b
 #pragma unroll
     for (int e = 0; e < 8; ++e) r[e] = (s > 0.f ? fminf(fmaxf(__fdiv_rn(x[e] - b, s), 0.f), 100.f) : 0.f) + MAGIC;
   }
-  uint32_t w = 0;
+  // as integers r is 0x4b400000 and 16 .. 31; the multiples of 0x4b400010 that are summed with the codes are taken off at the end (modulo 2^32)
+  uint32_t w = 0, extra = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const int c = min(max(__float_as_int(r[e]), 0x4b400010), 0x4b40001f) & 15;      // (16 .. 31, less 16)
-    w |= (uint32_t)c << (4 * (e / 2) + 16 * (e % 2));
+    const uint32_t place = 1u << (4 * (e / 2) + 16 * (e % 2));
+    w += (uint32_t)min(max(__float_as_int(r[e]), 0x4b400010), 0x4b40001f) * place;
+    extra += 0x4b400010u * place;
   }
-  return w;
+  return w - extra;
 }
 }  // namespace kv4
 
@@ -117,7 +125,7 @@ __global__ void __launch_bounds__(KV4_THREADS) kv4_store_kernel(const bf16 *k, l
 #pragma unroll
       for (int o = 1; o < 4; o <<= 1) { lo2 = __hmin2(lo2, __shfl_xor_sync(warp_lanes, lo2, o)); hi2 = __hmax2(hi2, __shfl_xor_sync(warp_lanes, hi2, o)); }
       const float lo = fminf(__low2float(lo2), __high2float(lo2)), hi = fmaxf(__low2float(hi2), __high2float(hi2));
-      const bf16 s16 = __float2bfloat16_rn(__fdiv_rn(hi - lo, 15.f));
+      const bf16 s16 = __float2bfloat16_rn(kv4::fifteenth(hi - lo));
       const float s = __bfloat162float(s16);
       const bf16 b16 = __float2bfloat16_rn(lo - 16.f * s);
       const uint32_t code = kv4::codes8(x, s, __bfloat162float(b16));
