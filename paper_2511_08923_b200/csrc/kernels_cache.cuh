@@ -74,10 +74,10 @@ __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float s, float b
 }  // namespace kv4
 
 // Rows of K and V to the slots (64 page + place) that the page map gave them; a slot outside the pool is skipped.  Four threads share a group of 32
-// dimensions, eight each; a thread takes the same place of K and V, so that two loads are on their way at once.  What bounds it: memory, 2.6 bytes an element;
-// most instructions go into the codes.
+// dimensions, eight each; a thread takes the same place of K and V, so that two loads are on their way at once.  Instructions bound it, most of
+// them for the codes (20001 rows of 8 heads of 128: 39 us, 108 MB; 44 with the five blocks per SM that fit without asking for six).
 template <int HD>
-__global__ void __launch_bounds__(KV4_THREADS) kv4_store_kernel(const bf16 *k, long long k_stride, const bf16 *v, long long v_stride, const int32_t *slots,
+__global__ void __launch_bounds__(KV4_THREADS, 6) kv4_store_kernel(const bf16 *k, long long k_stride, const bf16 *v, long long v_stride, const int32_t *slots,
                                                                 int n_rows, int heads, uint8_t *k_pages, uint8_t *v_pages, int n_pages) {
   constexpr int PER_HEAD = HD / 8;
   const int per_row = heads * PER_HEAD;                // (a multiple of eight: the four threads of a group lie in one warp, full or not)
