@@ -16,7 +16,7 @@ constexpr int PAGE = 64, GROUP = 32;
 __host__ __device__ constexpr int code_bytes(int hd) { return PAGE * hd / 2; }
 __host__ __device__ constexpr int record_bytes(int hd) { return PAGE * (hd / 2 + hd / GROUP * 4); }
 __host__ __device__ constexpr int word_at(int place, int w) { return (w / 4 * PAGE + place) * 16 + w % 4 * 4; }      // of dimensions 8 w .. 8 w + 7
-constexpr float LARGEST = 8.507059173023462e37f;      // 2^126: twice that, and a base 16 scales away, are still finite
+constexpr float LARGEST = 8.507059173023462e37f;      // 2^126: twice that, and a base 16 scales away (-1.57 * 2^127), are still finite; their difference need not be (see codes8)
 
 // Four pairs of values (dimensions 8 w .. 8 w + 7) of word `w`; ss = (s, s), bb = (b, b).
 __device__ __forceinline__ uint32_t pair_of(uint32_t shifted, uint32_t ss, uint32_t bb) {
@@ -58,8 +58,9 @@ __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float s, float b
     r[e] = fmaf(fmaf(-q, s, y), inv, q) + MAGIC;
   }
   if (!(s > 1e-30f && s < 1e30f)) {                    // where remainders or the reciprocal leave the range of normal numbers; and a scale of 0, which gives code 0
+    const float part = s < 1.f ? 1.f : 0.25f;          // (x - b reaches 2^128.05: of large numbers quarters are divided, which changes no quotient)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = (s > 0.f ? fminf(fmaxf(__fdiv_rn(x[e] - b, s), 0.f), 100.f) : 0.f) + MAGIC;
+    for (int e = 0; e < 8; ++e) r[e] = (s > 0.f ? fminf(fmaxf(__fdiv_rn(fmaf(x[e], part, -(b * part)), s * part), 0.f), 100.f) : 0.f) + MAGIC;
   }
   // as integers r is 0x4b400000 and 16 .. 31; the multiples of 0x4b400010 that are summed with the codes are taken off at the end (modulo 2^32)
   uint32_t w = 0, extra = 0;
