@@ -2,6 +2,7 @@
 // pages with a sliding window.  (The kernels that read them fast: attn_few.cuh, attn_tc.cuh.)
 #pragma once
 #include "common.cuh"
+#include "sm100_ptx.cuh"
 
 // ---- rows in 4 bits --------------------------------------------------------------------
 // Every 32 dimensions of a head (a group) have a scale s = bf16((max - min) / 15) and a base b = bf16(min - 16 s).  An element is held as
@@ -48,19 +49,29 @@ __device__ __forceinline__ float fifteenth(float d) {
 }
 // The codes of eight elements as a word.  The quotient is corrected once by its exact remainder, which makes it the correctly rounded one (Markstein: the
 // reciprocal is correctly rounded and s, a bf16 number, not the largest of its binade), so that ties, of which numbers of eight bits have many, are ties.
+// Nothing else must be one.  A distance y = x - b > 0 that is off a border between two codes is so by a unit of its last place at least, which is more than
+// half a unit of the quotient's.  But where x - b does not fit 32 bits, rounding it can bring it onto a border.  With s in [2^e, 2^(e+1)) borders are multiples
+// of 2^(e-8) (b, near -16 s or further out wherever there is an x that small, and s have eight bits), and y is below 2^(e+6), so that this takes an x within
+// 2^(e-18) of a border at 0.  A tie there goes to the even one of its neighbours: where that is the upper one distances are rounded down, otherwise up, and
+// what lands on the border goes the way that it should have gone without.
 __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float s, float b) {
+  using namespace sm100;
   constexpr float MAGIC = 12582912.f;                  // 1.5 * 2^23: adding it rounds to an integer, ties to even, which are then the low bits
   const float inv = __frcp_rn(s);
   float r[8];                                          // the quotients, rounded, + MAGIC
+  // rounded up, a distance is the negative of its negative rounded down: all signs are `up`'s
+  const uint32_t up = ~__float_as_uint(fmaf(-b, inv, -0.5f) + MAGIC) << 31;       // (the integer below a border at 0 is even)
+  auto sign = [&](float v) { return __uint_as_float(__float_as_uint(v) ^ up); };
+  const float one = sign(1.f), nb = sign(-b), ss = sign(s), si = sign(inv);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float y = x[e] - b, q = y * inv;
-    r[e] = fmaf(fmaf(-q, s, y), inv, q) + MAGIC;
+  for (int e = 0; e < 8; e += 2) {                     // (in pairs: 42.5 us one by one)
+    const f32x2 y = fma2_down(pack2(x[e], x[e + 1]), pack2(one, one), pack2(nb, nb)), q = mul2(y, pack2(si, si));
+    unpack2(add2(fma2(fma2(q, pack2(-ss, -ss), y), pack2(si, si), q), pack2(MAGIC, MAGIC)), r[e], r[e + 1]);
   }
   if (!(s > 1e-30f && s < 1e30f)) {                    // where remainders or the reciprocal leave the range of normal numbers; and a scale of 0, which gives code 0
     const float part = s < 1.f ? 1.f : 0.25f;          // (x - b reaches 2^128.05: of large numbers quarters are divided, which changes no quotient)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = (s > 0.f ? fminf(fmaxf(__fdiv_rn(fmaf(x[e], part, -(b * part)), s * part), 0.f), 100.f) : 0.f) + MAGIC;
+    for (int e = 0; e < 8; ++e) r[e] = (s > 0.f ? fminf(fmaxf(__fdiv_rn(__fmaf_rd(x[e], one * part, nb * part), ss * part), 0.f), 100.f) : 0.f) + MAGIC;
   }
   // as integers r is 0x4b400000 and 16 .. 31; the multiples of 0x4b400010 that are summed with the codes are taken off at the end (modulo 2^32)
   uint32_t w = 0, extra = 0;
@@ -76,7 +87,7 @@ __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float s, float b
 
 // Rows of K and V to the slots (64 page + place) that the page map gave them; a slot outside the pool is skipped.  Four threads share a group of 32
 // dimensions, eight each; a thread takes the same place of K and V, so that two loads are on their way at once.  Instructions bound it, most of
-// them for the codes (20001 rows of 8 heads of 128: 39 us, 108 MB; 44 with the five blocks per SM that fit without asking for six).
+// them for the codes (20001 rows of 8 heads of 128: 40 us, 108 MB; 44 with the five blocks per SM that fit without asking for six, which spill 20 bytes a thread).
 template <int HD>
 __global__ void __launch_bounds__(KV4_THREADS, 6) kv4_store_kernel(const bf16 *k, long long k_stride, const bf16 *v, long long v_stride, const int32_t *slots,
                                                                 int n_rows, int heads, uint8_t *k_pages, uint8_t *v_pages, int n_pages) {

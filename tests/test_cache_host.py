@@ -92,3 +92,45 @@ def test_visibility_by_cases():
     assert np.nonzero(v[2])[0].tolist() == [0, 1, 2, 8, 9, 10]              # block 0, slot 0: position 11
     assert np.nonzero(v[5])[0].tolist() == [0, 1, 2, 10, 11]                # block 1, slot 1: position 13
     assert H.visible(10, 2, True, 0, 0, 12)[5].sum() == 12
+
+
+def _recorder(hq=4, hkv=2, hd=64):
+    """A binding object whose library calls are recorded instead of made; CPU (and meta) tensors count as on its device."""
+    from types import SimpleNamespace
+    t = Tidar.__new__(Tidar)
+    t._index, t.shape, t.lib, t.ctx, t.calls = -1, SimpleNamespace(n_q_heads=hq, n_kv_heads=hkv, head_dim=hd), binding.load(), None, []
+    t._on_device = lambda entry, *args: t.calls.append(args)
+    return t
+
+
+def test_the_binding_refuses_numbers_that_the_library_cannot_hold():
+    """Integers are 32 bits in the library: 2^32 + 5 would arrive there as 5."""
+    t, bf = _recorder(), torch.bfloat16
+    q, out, n, table = torch.zeros(1, 4, 64, dtype=bf), torch.zeros(1, 256, dtype=bf), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 3, dtype=torch.int32)
+    pools = {t.attention_kv4: torch.zeros(3, 2, kv4_page_bytes(64), dtype=torch.uint8), t.attention_window: torch.zeros(3, 2, 64, 64, dtype=bf)}
+    for call, pool in pools.items():
+        for good in (dict(window=0), dict(window=2 ** 31 - 1, sinks=2 ** 31 - 1)):
+            t.calls.clear()
+            call(q, pool, pool, table, n, None, None, out, 1, 1, **good)
+            args = t.calls[0][0]._obj
+            assert args.window == good["window"] and args.sinks == good.get("sinks", 0)
+        t.calls.clear()
+        for bad in (dict(window=2 ** 31), dict(window=2 ** 32 + 5), dict(window=-2 ** 31 - 1), dict(window=9, sinks=2 ** 32), dict(window=9, sinks=-2 ** 32)):
+            with pytest.raises(ValueError):
+                call(q, pool, pool, table, n, None, None, out, 1, 1, **bad)
+    many, one = 2 ** 32 + 5, lambda k: torch.zeros(k, dtype=torch.int32)
+    meta = lambda *s, dtype=torch.int32: torch.empty(*s, dtype=dtype, device="meta")
+    for free, slots, wide in ((one(4), meta(many), table), (meta(many), one(4), table), (one(4), one(4), meta(1, many))):
+        with pytest.raises(ValueError):
+            t.page_map(n, n, n, free, wide, one(1), one(2), slots, one(3))
+    rows, pool = meta(many, 2, 64, dtype=bf), meta(3, 2, kv4_page_bytes(64), dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        t.kv4_store(rows, rows, meta(many), pool, pool)
+    with pytest.raises(ValueError):
+        t.kv4_load(pool, pool, meta(many), rows, rows)
+    pool = meta(many, 2, kv4_page_bytes(64), dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        t.kv4_store(meta(7, 2, 64, dtype=bf), meta(7, 2, 64, dtype=bf), one(7), pool, pool)
+    assert not t.calls
+    t.page_map(n, n, n, one(4), table, one(1), one(2), one(4), one(3))
+    assert len(t.calls) == 1

@@ -37,3 +37,24 @@ def test_codes_at_the_top_of_the_range():
     ends = np.tile([[-top, top]], (len(values), 1))
     _groups_are_stored_as_stated(np.concatenate([ends, values], 1))
     _groups_are_stored_as_stated(np.concatenate([ends * [1, 0.5], np.clip(values, -top, top / 2)], 1))
+
+
+@pytest.mark.parametrize("exponent", [-100, -98, -60, 0, 50, 90, 105])
+@pytest.mark.parametrize("mantissa", [1.0, 1.5])
+def test_codes_of_elements_next_to_the_border_between_two(exponent, mantissa):
+    """Where an element is far smaller than its group's scale, its distance from the base does not fit 32 bits; a border lies at 0 for these groups, so that such
+    an element's sign alone decides (0 itself is a tie)."""
+    s = mantissa * 2.0 ** exponent
+    groups = []
+    for r in range(16, 31):                                      # base -(r + 1/2) s: the border between r and r + 1 is at 0
+        lo = -(r - 15.5) * s
+        g = np.linspace(lo, lo + 15 * s, 32)
+        g = H.bf16_round(g)
+        for tiny in ([2.0 ** -25, 2.0 ** -30 * (1 + 2.0 ** -7), 2.0 ** -33], [2.0 ** -17, 2.0 ** -18 * (1 + 2.0 ** -7), 2.0 ** -18], [2.0 ** -19, 2.0 ** -19 * (1 + 2.0 ** -7), 2.0 ** -20],
+                     [2.0 ** -20 * (1 + 2.0 ** -7), 2.0 ** -21, 2.0 ** -22]):
+            tiny = np.array(tiny) * 2.0 ** exponent
+            g[3:10] = np.concatenate([tiny, -tiny, [0.0]])
+            groups.append(g.copy())
+            c, scale, base = H.quantise(g)
+            assert scale == s and base == -(r + 0.5) * s and len(set(c[3:9].tolist())) == 2
+    _groups_are_stored_as_stated(groups)
