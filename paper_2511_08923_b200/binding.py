@@ -454,9 +454,12 @@ class Tidar:
     @staticmethod
     def _length(name, x, dim=0):
         try:
-            return x.shape[dim]
+            n = x.shape[dim]
         except (AttributeError, IndexError):
             raise ValueError(f"{name} must be a tensor of at least {dim + 1} dimensions") from None
+        if n > 0x7fffffff:                             # (the library's integers are 32 bits, and ctypes cuts without a word)
+            raise ValueError(f"{name} has {n} entries; the library takes at most 2^31 - 1")
+        return n
 
     def page_map(self, seq_len, n_new, held, free_pages, page_table, held_out, row_start, slots, counts, free_begin=None):
         """Page table entries and slots for the rows that sequences are about to get (see tidar_page_map).
@@ -491,6 +494,8 @@ class Tidar:
 
     def _attention_cache(self, entry, record, dtype, q, k_pages, v_pages, page_table, seq_len, k_local, v_local, out, n_seqs, k, window, sinks):
         hq, hkv, hd, bf16, tensor = self.shape.n_q_heads, self.shape.n_kv_heads, self.shape.head_dim, torch.bfloat16, self._tensor
+        if not (-0x80000000 <= window <= 0x7fffffff and -0x80000000 <= sinks <= 0x7fffffff):       # (n_seqs and k are what the shapes below say)
+            raise ValueError(f"window and sinks must fit 32 bits, not {window} and {sinks}")
         blocks = k_local is not None or v_local is not None
         rows, n_pages, width = n_seqs * k * (k + 1 if blocks else 1), self._length("k_pages", k_pages), self._length("page_table", page_table, 1)
         pool = (n_pages, hkv) + record
