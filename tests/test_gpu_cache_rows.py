@@ -58,3 +58,18 @@ def test_codes_of_elements_next_to_the_border_between_two(exponent, mantissa):
             c, scale, base = H.quantise(g)
             assert scale == s and base == -(r + 0.5) * s and len(set(c[3:9].tolist())) == 2
     _groups_are_stored_as_stated(groups)
+
+
+def test_codes_of_very_small_groups():
+    """Scales and spreads on both sides of 1e-30, below which quotients are divisions; numbers of few bits among them, so that ties are."""
+    rng = np.random.default_rng(3)
+    groups = []
+    for exponent in range(-112, -90):
+        x = rng.standard_normal((12, 32))
+        x[6:] = np.rint(x[6:] * 8) / 4
+        x[np.abs(x) < 2.0 ** -12] = 0                            # (normal numbers, for the plain statement)
+        groups.append(H.bf16_round(x * 2.0 ** exponent))
+    groups = np.concatenate(groups)
+    s = H.quantise(groups)[1]
+    assert s.min() < 2.0 ** -110 and (s > 1.2e-30).any() and (s > 1e-32).any()
+    _groups_are_stored_as_stated(groups)
