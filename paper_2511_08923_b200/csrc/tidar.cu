@@ -258,8 +258,9 @@ void layout(tidar_ctx &x, void *arena, size_t *bytes) {
 // kernel of the stream is still running and synchronises itself with pdl_wait(); only kernels that call
 // pdl_wait() before they touch produced data may be launched this way.  Between a projection and the small kernel
 // behind it (norm, RoPE) an ordinary dependency costs 2.3 - 4 us, this one 1.0 - 1.5.  What makes it pay is that the
-// kernels fit beside one another: all ask for the same split of the SM's memory (an SM changes its split only when it is
-// empty; see init_tensor_core_path).
+// kernels fit beside one another: all of a step ask for the same split of the SM's memory (an SM changes its split only when it is
+// empty; see init_tensor_core_path.  The plan, merge and row kernels of calls over a caller's pages do not: what it would bring them was not measured).
+// pdl_wait() also makes all that earlier kernels of the stream wrote visible to plain loads, the non-coherent kind excepted.
 template <typename... KP, typename... AP>
 inline void launch_pdl_cluster(unsigned cluster, void (*kernel)(KP...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, AP &&...args) {
   cudaLaunchConfig_t cfg{};
@@ -724,7 +725,8 @@ void launch_attention(tidar_ctx *c, const bf16 *Q, const bf16 *Kp, const bf16 *V
 }
 
 // 4-bit pages: sequences of so few rows per KV head go through attn_few_kernel (24 sequences of up to 9 k positions, 32/8 heads: 16 rows 82 us there and 164 through
-// the 128-row tiles, 32 rows 152 and 164, 48 rows 217 and 165; one of 2 k positions 16.3 / 15.0, 16.9 / 15.0, 17.1 / 15.1).
+// the 128-row tiles, 32 rows 152 and 164, 48 rows 217 and 165; one of 2 k positions 16.3 / 15.0, 16.9 / 15.0, 17.1 / 15.1).  The rule is made for the work that
+// takes long: the lengths are on the device, and 16 to 32 rows over little context pay up to 2 us for it.
 bool few_rows(const tidar_ctx *c, const WindowRows &w) { return w.rows() * (c->cfg.n_q_heads / c->cfg.n_kv_heads) <= 2 * attn_few::MAX_ROWS; }
 
 template <int HD, int N8, bool MANY>
@@ -741,7 +743,7 @@ void launch_few_rows(tidar_ctx *c, attn_few::Args &a, int n8, bool many) {
 }
 
 // Calls over a caller's pages on the tensor cores: as tidar_attention's (see attention_direct), except that a tile's pages are those of its window, and that
-// 4-bit pages have no instance of one stream (its warps and the four that turn codes into tiles would not fit an SM twice).
+// 4-bit pages have no instance of one stream (its warps and the eight that turn codes into tiles would not fit an SM twice).
 template <int CACHE>
 int launch_cache_attention(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
   const WindowRows &w = x.rows;
@@ -753,9 +755,11 @@ int launch_cache_attention(tidar_ctx *c, const CacheArgs &x, int n_seqs) {
   DirectPlan d = attention_direct(c, n_seqs, T, n_pages);
   if (CACHE == attn_tc::KV4 && d.streams == 1) d.streams = 0;
   // One sequence: its tiles have about the same pages, so the SMs share them evenly without a plan where that comes to two parts of each or more (32/8 heads, 272
-  // rows, a window of 4 k: 37.0 us planned, 33.9 not; 4 bits, 32 k positions 224 and 215); uncut while a plan that cuts pairs would gain no more than it costs.
+  // rows, a window of 4 k: 37.0 us planned, 33.9 not; 4 bits, 32 k positions 224 and 215); uncut while a plan that cuts pairs would gain no more than it costs
+  // (32/8 heads, 330 causal rows, 88 tiles, bf16: 37 pages 31.7 us planned and 28.5 not, 45 pages 33.8 and 33.5, 53 pages 35.7 and 37.3; 120 tiles, 70 pages
+  // 54.2 and 48.7.  In 4 bits 34.0 and 36.4 at 37 pages; up to 31 pages attention_direct has no plan anyway).
   const int tiles = n_seqs * ((T + spt - 1) / spt) * x.Hkv;
-  if (!d.streams && n_seqs == 1 && (2 * tiles <= c->n_sms || (tiles <= c->n_sms && n_pages <= (CACHE == attn_tc::KV4 ? 24 : 45)))) d = {2, std::min<int>(attn_tc::MAX_SPLITS, c->n_sms / tiles), 1};
+  if (!d.streams && n_seqs == 1 && (2 * tiles <= c->n_sms || (CACHE == attn_tc::WINDOW && tiles <= c->n_sms && n_pages <= 45))) d = {2, std::min<int>(attn_tc::MAX_SPLITS, c->n_sms / tiles), 1};
   attn_tc::PlanArgs plan{};
   if (!d.streams) {
     c->split_keys = may_split((int)std::min<long long>((long long)n_pages * 64, INT32_MAX)); c->attn_cluster = 1;
